@@ -17,6 +17,13 @@
  *                       several blocks, for few rows (decode, Sec. 2.2)
  *   janus_sparse_attn_fp8kv  MLA attention over an FP8 KV cache (Sec. 5.1)
  *
+ * Around them, what makes their inputs, and the dense layers beside them:
+ *
+ *   janus_page_grow     page tables and slot maps of the appended tokens
+ *   janus_rope          rotary positions of queries, to bf16, fp32 or fp8
+ *   janus_kv_append     the appended tokens' rows into the caches
+ *   janus_prefix_attn   dense attention for a batch with a shared prefix
+ *
  * Running index_scores + topk + page_demand on a predicted indexer query
  * (an earlier layer's hidden state through this layer's indexer) gives the
  * predicted union of Eq. (2).
@@ -383,6 +390,153 @@ int janus_sparse_attn_fp8kv(const janus_batch *b,
                             void *out, janus_dtype out_dt, float *lse,
                             int num_splits, void *workspace, size_t *workspace_bytes,
                             void *stream);
+
+/*
+ * Page tables and slot maps (paged KV caches; the appended tokens' KV is
+ * produced in HBM, Sec. 2.2).  Gives every session the pages that its appended
+ * tokens need beyond those of its history, from a list of free pages, and every
+ * appended token the row of the pool that its entry goes to.
+ *
+ * With H_b = M_b >> e history entries, C_b = (M_b + N_b) >> e and ps = page_size,
+ * session b holds ceil(H_b / ps) pages and needs ceil(C_b / ps).  The new ones
+ * are the next of free_list, sessions in order and pages in order.  Token i of
+ * session b completes entry c = ((M_b+i+1) >> e) - 1 if 2^e divides M_b+i+1 (every
+ * token does at token granularity); its slot is
+ * page_table[b, c / ps] * ps + c % ps, and -1 if it completes none.
+ *   free_list   device [free_len] int32: physical pages, each once
+ *   free_head   device [1] int32: entries of free_list that are taken already
+ *               (>= 0), or NULL for 0; not inside counts
+ *   page_table  device [B, pt_ld] int32, in and out: the pages of the history are
+ *               read, the new pages' entries written, all others left as they are
+ *   slots       device [total_q] int64
+ *   counts      device [3] int32: {pages taken, free_head after them, pages
+ *               that the list was short of}
+ * Pages that the list is short of are not written to the table and their
+ * tokens' slots are -1: such a batch must not go on to attention before pages
+ * are freed.  Rows from q_start[B] on get slot -1.
+ */
+int janus_page_grow(const janus_batch *b, int page_size,
+                    const int32_t *free_list, int free_len, const int32_t *free_head,
+                    int32_t *page_table, int pt_ld, int64_t *slots, int32_t *counts,
+                    void *stream);
+
+/*
+ * Rotary positions.  Of every head, `dim` elements from `offset` on are taken in
+ * pairs and turned by t = position * inv_freq[pair]:
+ *
+ *   (x_a, x_b) -> magnitude * (x_a cos t - x_b sin t, x_b cos t + x_a sin t)
+ *
+ * Pair j is elements (j, j + dim/2) with JANUS_ROTARY_HALVES and (2j, 2j+1) with
+ * JANUS_ROTARY_INTERLEAVED.  inverse != 0 turns by -t: the transpose, which
+ * takes the gradient of the outputs to the gradient of the inputs.
+ */
+typedef enum { JANUS_ROTARY_HALVES = 0, JANUS_ROTARY_INTERLEAVED = 1 } janus_rotary_layout;
+
+typedef struct {
+    int32_t dim;               /* even, 2 .. 1024                                  */
+    int32_t offset;            /* >= 0, offset + dim <= the head's size            */
+    int32_t layout;            /* janus_rotary_layout                              */
+    int32_t inverse;           /* 0, or the transpose                              */
+    float magnitude;           /* factor of the rotated elements                   */
+    const double *inv_freq;    /* device [dim/2]                                   */
+    const int32_t *positions;  /* device [total_q], or NULL for M_b + i            */
+} janus_rotary;
+
+/*
+ * Frequencies of a rotary embedding (host only: inv_freq is host memory, dim/2
+ * doubles; nothing is enqueued).  Pair j turns base^(-2j/dim) a position.
+ * JANUS_SCALING_LINEAR divides all frequencies by factor.  JANUS_SCALING_YARN
+ * (Peng et al., arXiv 2309.00071) keeps those that make more than beta_fast
+ * turns over original_ctx positions, divides those that make fewer than
+ * beta_slow, goes from one to the other linearly in j, and sets magnitude to
+ * 0.1 ln(factor) + 1 (else 1).  The arguments that a kind does not use are
+ * ignored (factor must be >= 1 all the same).
+ */
+typedef enum { JANUS_SCALING_NONE = 0, JANUS_SCALING_LINEAR = 1, JANUS_SCALING_YARN = 2 } janus_rotary_scaling;
+
+int janus_rotary_frequencies(int dim, double base, double factor, int scaling, int original_ctx,
+                             double beta_fast, double beta_slow, double *inv_freq, float *magnitude);
+
+/*
+ * Rotary positions of the appended tokens' heads (queries of the indexer and of
+ * attention; keys that stay out of a cache).
+ *   x      device [total_q, heads, size], x_dt JANUS_F32 or JANUS_BF16; strides in
+ *          elements between tokens and heads, a head's elements adjacent
+ *   out    device, the same shape with its own strides, out_dt JANUS_F32,
+ *          JANUS_BF16 or JANUS_FP8_E4M3.  It is x itself (same type and strides:
+ *          only the rotated elements are read and written) or shares no
+ *          element with it.
+ *   out_scale  device [total_q] fp32 for fp8, NULL otherwise
+ * fp8 outputs are quantised over all heads of a token, as janus_index_scores
+ * takes its queries: out_scale = max(largest finite magnitude, 1e-12) / 448 and
+ * out = the nearest e4m3 of value / out_scale (infinities as the largest value, NaN as
+ * NaN).  Angles are reduced in fp64, the rotation is fp32, and results are
+ * rounded to out_dt once.  Rows from q_start[B] on are left as they are.
+ * heads * size up to 2^24 (else JANUS_ERR_UNSUPPORTED).
+ */
+int janus_rope(const janus_batch *b, const janus_rotary *r, const void *x, janus_dtype x_dt,
+               int64_t x_row_stride, int64_t x_head_stride, int heads, int size,
+               void *out, janus_dtype out_dt, int64_t out_row_stride, int64_t out_head_stride,
+               float *out_scale, void *stream);
+
+/*
+ * Rows of the appended tokens into a cache: the paged KV pools, or the ragged
+ * indexer keys.  A token's row of `size` elements is x's, with the elements
+ * [offset, offset + dim) rotated; given x_rot, those come from x_rot and x holds
+ * the others only (latent and rotary parts of an MLA row from two tensors).
+ *   r        the rotation, or NULL for none (x_rot must be NULL then)
+ *   x        device [total_q, size] (with x_rot: [total_q, size - dim], NULL if that
+ *            is empty), x_dt JANUS_F32 or JANUS_BF16, x_row_stride in elements
+ *   x_rot    device [total_q, dim] of the same type, or NULL
+ *   rows     device [total_q] int64: the output row of each token, as
+ *            janus_page_grow's slots; rows outside [0, num_rows) are skipped.
+ *            No row twice.  NULL: row ctx_start[b] + c of the entry c that the
+ *            token completes (the key arrays of janus_index_scores).
+ *   out      device, num_rows rows of out_row_bytes bytes, whose first `size` elements
+ *            are written; the other rows, and bytes behind a row, stay
+ *   out_dt   JANUS_F32, JANUS_BF16 or JANUS_FP8_E4M3.  fp8 rows are quantised like
+ *            janus_rope's; their scale goes to out_scale[row] (device
+ *            [num_rows] fp32), or with out_scale == NULL to byte `size` of the
+ *            row (janus_sparse_attn_fp8kv's rows: size 576, 592 bytes).
+ * A scale in the row needs size and out_row_bytes in multiples of 4 and out
+ * 4-byte aligned (else JANUS_ERR_UNSUPPORTED), as does size up to 2^24.  Rows from
+ * q_start[B] on are skipped.
+ */
+int janus_kv_append(const janus_batch *b, const janus_rotary *r, const void *x, janus_dtype x_dt,
+                    int64_t x_row_stride, const void *x_rot, int64_t x_rot_stride, int size,
+                    const int64_t *rows, int64_t num_rows, void *out, janus_dtype out_dt,
+                    int64_t out_row_bytes, float *out_scale, void *stream);
+
+/*
+ * Dense causal attention of the appended tokens over all cached ids, for a
+ * batch whose sessions begin with the same prefix_len ids (a system prompt that
+ * many agents share): the same attention as janus_sparse_attn with S_i = {0 ..
+ * M_b+i} (entries: 0 .. ((M_b+i+1) >> e) - 1).
+ *
+ * Ids below prefix_len have the same rows in every session: page_table's first
+ * ceil(prefix_len / page_size) entries of each session that reads them give
+ * pages with the same contents there (usually the same pages; the page the
+ * prefix ends in may be a copy).  Where that pays, rows of different
+ * sessions meet the prefix's keys together, through table row 0, and their own ids apart,
+ * joined by their maxima and sums.  prefix_len = 0 is any ragged batch.
+ *   prefix_len      0 .. max_ctx, in ids
+ *   q, pools, strides, page_table, softmax_scale, out, lse: as janus_sparse_attn
+ *   workspace, workspace_bytes: as janus_sparse_attn_split
+ * Shapes: MLA (dqk = 576, dv = 512, v_pool == k_pool, equal strides) and MQA
+ * (dqk = dv = 128), each with 1 <= Hq <= 128, q and pools 16-byte aligned and
+ * row strides in multiples of 8, total_q * Hq < 2^31; else JANUS_ERR_UNSUPPORTED.  A
+ * workspace that is used must be 16-byte aligned, and out 4-byte aligned (else
+ * JANUS_ERR_UNSUPPORTED).  A token with no candidate gets out = 0 and lse = -inf.  Rows from
+ * q_start[B] on are left as they are.  Ids that a token does not attend to
+ * do not touch its result, whatever their rows hold.
+ */
+int janus_prefix_attn(const janus_batch *b, const void *q, int Hq, int dqk, int dv,
+                      const void *k_pool, const void *v_pool,
+                      int64_t k_row_stride, int64_t v_row_stride,
+                      const int32_t *page_table, int pt_ld, int page_size,
+                      int prefix_len, float softmax_scale,
+                      void *out, janus_dtype out_dt, float *lse,
+                      void *workspace, size_t *workspace_bytes, void *stream);
 
 /* Static description of a status code. */
 const char *janus_status_string(int status);

@@ -41,6 +41,18 @@ class _Batch(ctypes.Structure):
     ]
 
 
+class _Rotary(ctypes.Structure):
+    _fields_ = [
+        ("dim", ctypes.c_int32),
+        ("offset", ctypes.c_int32),
+        ("layout", ctypes.c_int32),
+        ("inverse", ctypes.c_int32),
+        ("magnitude", ctypes.c_float),
+        ("inv_freq", ctypes.c_void_p),
+        ("positions", ctypes.c_void_p),
+    ]
+
+
 _lib = None
 
 
@@ -67,7 +79,14 @@ def lib():
         L.janus_sparse_attn_fp8kv.argtypes = [BP, P, i32, P, i64, P, i32, i32, P, i32, f32, P, i32, P, i32, P, SZ, P]
         L.janus_sparse_attn_split_noalloc.argtypes = [BP, P, i32, i32, i32, P, P, i64, i64, P, i32, i32, P, i32, f32,
                                                       P, i32, P, i32, P]
-        for f in ("janus_index_scores", "janus_topk", "janus_topk_sharded", "janus_page_demand",
+        RP, f64 = ctypes.POINTER(_Rotary), ctypes.c_double
+        L.janus_page_grow.argtypes = [BP, i32, P, i32, P, P, i32, P, P, P]
+        L.janus_rotary_frequencies.argtypes = [i32, f64, f64, i32, i32, f64, f64, P, ctypes.POINTER(f32)]
+        L.janus_rope.argtypes = [BP, RP, P, i32, i64, i64, i32, i32, P, i32, i64, i64, P, P]
+        L.janus_kv_append.argtypes = [BP, RP, P, i32, i64, P, i64, i32, P, i64, P, i32, i64, P, P]
+        L.janus_prefix_attn.argtypes = [BP, P, i32, i32, i32, P, P, i64, i64, P, i32, i32, i32, f32, P, i32, P, P, SZ, P]
+        for f in ("janus_page_grow", "janus_rotary_frequencies", "janus_rope", "janus_kv_append", "janus_prefix_attn",
+                  "janus_index_scores", "janus_topk", "janus_topk_sharded", "janus_page_demand",
                   "janus_predict_diff", "janus_sparse_attn", "janus_sparse_attn_split", "janus_index_scores_mxfp4",
                   "janus_sparse_attn_fp8kv", "janus_sparse_attn_split_noalloc"):
             getattr(L, f).restype = ctypes.c_int
@@ -338,4 +357,253 @@ def sparse_attn_fp8kv(batch: Batch, q, kv_pool, page_table, page_size: int, topk
     have = ctypes.c_size_t(workspace.numel() * workspace.element_size())
     rc = lib().janus_sparse_attn_fp8kv(*args, _ptr(workspace), ctypes.byref(have), _stream(stream))
     _check(rc, "janus_sparse_attn_fp8kv")
+    return out, lse
+
+
+_LAYOUTS = {"half": 0, "interleaved": 1}
+_SCALINGS = {None: 0, "linear": 1, "yarn": 2}
+
+
+def _device(what: str, *tensors) -> torch.device:
+    """The one device that all the tensors (None: absent) are on."""
+    dev = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda or (dev is not None and t.device != dev):
+            raise JanusError(f"{what}: tensors of one GPU expected")
+        dev = t.device
+    return dev
+
+
+def _want(what: str, name: str, t, dtype, *shape):
+    """t has this dtype, these sizes (None: any) and adjacent elements."""
+    if t.dtype != dtype or t.dim() != len(shape) or not t.is_contiguous() or any(
+            n is not None and n != m for n, m in zip(shape, t.shape)):
+        raise JanusError(f"{what}: {name} is to be a contiguous {dtype} tensor of shape "
+                         f"{tuple('any' if n is None else n for n in shape)}, not {t.dtype} {tuple(t.shape)}")
+
+
+def _launch(what: str, dev: torch.device, stream, fn, *args):
+    """fn(*args, stream) on dev, whatever device is current."""
+    s = torch.cuda.current_stream(dev) if stream is None else stream
+    if torch.cuda.current_device() == dev.index:
+        rc = fn(*args, ctypes.c_void_p(s.cuda_stream))
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args, ctypes.c_void_p(s.cuda_stream))
+    _check(rc, what)
+
+
+def rotary_frequencies(dim: int, base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0,
+                       original_ctx: int = 0, beta_fast: float = 32.0, beta_slow: float = 1.0):
+    """janus_rotary_frequencies: (float64 array [dim/2], magnitude); scaling is
+    None, "linear" or "yarn"."""
+    if scaling not in _SCALINGS:
+        raise JanusError(f"unknown scaling {scaling!r}")
+    freq = np.zeros(max(int(dim) // 2, 1), dtype=np.float64)
+    mag = ctypes.c_float(1.0)
+    _check(lib().janus_rotary_frequencies(int(dim), float(base), float(factor), _SCALINGS[scaling], int(original_ctx),
+                                          float(beta_fast), float(beta_slow), freq.ctypes.data, ctypes.byref(mag)),
+           "janus_rotary_frequencies")
+    return freq, float(mag.value)
+
+
+class Rotary:
+    """Rotary positions: dim elements of every head, from offset on, in pairs
+    (j, j + dim/2) (layout "half") or (2j, 2j + 1) ("interleaved").
+
+    Frequencies come from inv_freq (float64 [dim/2] on the GPU, with mscale as the
+    factor of the rotated elements) or from rotary_frequencies(dim, base,
+    scaling, factor, ...).  positions: int32 [total_q] on the GPU, or None for each
+    appended token's own.  inverse: the transpose (the gradient)."""
+
+    def __init__(self, dim: int, offset: int = 0, layout: str = "half", base: float = 10000.0,
+                 scaling: Optional[str] = None, factor: float = 1.0, original_ctx: int = 0, beta_fast: float = 32.0,
+                 beta_slow: float = 1.0, inv_freq=None, mscale: Optional[float] = None, inverse: bool = False,
+                 positions=None, device="cuda"):
+        if layout not in _LAYOUTS:
+            raise JanusError(f"unknown layout {layout!r}")
+        mag = 1.0
+        if inv_freq is None:
+            freq, mag = rotary_frequencies(dim, base, scaling, factor, original_ctx, beta_fast, beta_slow)
+            inv_freq = torch.from_numpy(freq).to(device)
+        _want("Rotary", "inv_freq", inv_freq, torch.float64, int(dim) // 2)
+        if positions is not None:
+            _want("Rotary", "positions", positions, torch.int32, None)
+        _device("Rotary", inv_freq, positions)
+        self.inv_freq, self.positions = inv_freq, positions
+        self.mscale = float(mag if mscale is None else mscale)
+        self.dim, self.offset, self.layout = int(dim), int(offset), layout
+        self.c = _Rotary(self.dim, self.offset, _LAYOUTS[layout], int(bool(inverse)), self.mscale, inv_freq.data_ptr(),
+                         None if positions is None else positions.data_ptr())
+
+    def inverted(self) -> "Rotary":
+        """The transpose of this rotation."""
+        return Rotary(self.dim, self.offset, self.layout, inv_freq=self.inv_freq, mscale=self.mscale,
+                      inverse=not self.c.inverse, positions=self.positions)
+
+    def _check(self, what: str, batch: "Batch"):
+        if self.positions is not None and self.positions.numel() < batch.total_q:
+            raise JanusError(f"{what}: {self.positions.numel()} positions for {batch.total_q} tokens")
+
+    @property
+    def ref(self):
+        return ctypes.byref(self.c)
+
+
+def page_grow(batch: Batch, page_size: int, free_list, page_table, free_head=None, out=None, stream=None):
+    """janus_page_grow: extends page_table [B, pt_ld] (int32, in place) by the
+    pages the appended tokens need, off free_list (int32) from free_head (int32 [1],
+    None: 0) on.  Returns (page_table, slots [total_q] int64, counts [3] int32 =
+    pages taken, the next free_head, pages short); out = (slots, counts) to
+    write those tensors."""
+    what = "janus_page_grow"
+    if out is None:
+        out = (torch.empty(batch.total_q, dtype=torch.int64, device=page_table.device),
+               torch.empty(3, dtype=torch.int32, device=page_table.device))
+    slots, counts = out
+    dev = _device(what, page_table, free_list, free_head, slots, counts, batch.q_start)
+    _want(what, "page_table", page_table, torch.int32, batch.c.num_seqs, None)
+    _want(what, "free_list", free_list, torch.int32, None)
+    _want(what, "slots", slots, torch.int64, batch.total_q)
+    _want(what, "counts", counts, torch.int32, 3)
+    if free_head is not None and (free_head.dtype != torch.int32 or free_head.numel() != 1):
+        raise JanusError(f"{what}: free_head is to be one int32")
+    # an empty tensor has no address
+    _launch(what, dev, stream, lib().janus_page_grow, batch.ref, int(page_size), _ptr(free_list),
+            int(free_list.numel()), _ptr(free_head), _ptr(page_table), _table(batch, page_table, page_size),
+            _ptr(slots) if batch.total_q else _ptr(counts), _ptr(counts))
+    return page_table, slots, counts
+
+
+_ROPE_OUT = {"f32": (JANUS_F32, torch.float32), "bf16": (JANUS_BF16, torch.bfloat16),
+             "fp8": (JANUS_FP8_E4M3, torch.uint8)}
+
+
+def _float_code(what: str, name: str, t) -> int:
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise JanusError(f"{what}: {name} is to be float32 or bfloat16, not {t.dtype}")
+    return JANUS_F32 if t.dtype == torch.float32 else JANUS_BF16
+
+
+def rope(batch: Batch, rotary: Rotary, x, out=None, out_dtype: Optional[str] = None, out_scale=None, stream=None):
+    """janus_rope: x [total_q, heads, size] (float32 or bfloat16, adjacent elements
+    in a head, any other strides) with its rotated elements turned.  Returns (out,
+    out_scale or None).
+
+    out: a tensor of x's shape, x itself to turn it in place, or None for a new
+    one; out_dtype "f32", "bf16" or "fp8" (None: out's, or x's).  fp8 outputs are e4m3
+    bytes (uint8, or float8_e4m3fn if given) with one scale per token."""
+    what = "janus_rope"
+    if x.dim() != 3 or x.shape[0] != batch.total_q:
+        raise JanusError(f"{what}: x is to be [{batch.total_q}, heads, size], not {tuple(x.shape)}")
+    xdt = _float_code(what, "x", x)
+    if out_dtype is None:
+        out_dtype = "f32" if (x if out is None else out).dtype == torch.float32 else (
+            "bf16" if (x if out is None else out).dtype == torch.bfloat16 else "fp8")
+    if out_dtype not in _ROPE_OUT:
+        raise JanusError(f"{what}: unknown out_dtype {out_dtype!r}")
+    odt, torch_dt = _ROPE_OUT[out_dtype]
+    if out is None:
+        out = torch.empty(tuple(x.shape), dtype=torch_dt, device=x.device)
+    if out.dtype != torch_dt and not (out_dtype == "fp8" and out.dtype == torch.float8_e4m3fn):
+        raise JanusError(f"{what}: out is {out.dtype}, not {out_dtype}")
+    if out.shape != x.shape or any(t.shape[2] > 1 and t.stride(2) != 1 for t in (x, out)):
+        raise JanusError(f"{what}: x and out are to have one shape and adjacent elements in a head")
+    if out_dtype == "fp8":
+        if out_scale is None:
+            out_scale = torch.empty(batch.total_q, dtype=torch.float32, device=x.device)
+        _want(what, "out_scale", out_scale, torch.float32, batch.total_q)
+    elif out_scale is not None:
+        raise JanusError(f"{what}: out_scale goes with fp8 outputs")
+    rotary._check(what, batch)
+    dev = _device(what, x, out, out_scale, batch.q_start, rotary.inv_freq)
+    if batch.total_q:
+        _launch(what, dev, stream, lib().janus_rope, batch.ref, rotary.ref, _ptr(x), xdt, x.stride(0), x.stride(1),
+                int(x.shape[1]), int(x.shape[2]), _ptr(out), odt, out.stride(0), out.stride(1), _ptr(out_scale))
+    return out, out_scale
+
+
+def kv_append(batch: Batch, x, out, rotary: Optional[Rotary] = None, x_rot=None, rows=None, out_scale=None,
+              size: Optional[int] = None, stream=None):
+    """janus_kv_append: the appended tokens' rows into a cache; returns out.
+
+    x [total_q, size] (float32 or bfloat16), or [total_q, size - rotary.dim] beside
+    x_rot [total_q, rotary.dim] (x None if that is empty).  rows: int64 [total_q]
+    output rows (page_grow's slots; outside the cache: skipped), or None for the
+    ragged key arrays of index_scores.  out [..., row]: float32, bfloat16, or e4m3
+    bytes (uint8 or float8_e4m3fn) with their scales in out_scale (float32, one
+    per row), or in the row behind its elements if that is None."""
+    what = "janus_kv_append"
+    given = x if x is not None else x_rot
+    if given is None or any(t is not None and (t.dim() != 2 or t.shape[0] != batch.total_q or t.dtype != given.dtype or
+                                               (t.shape[1] > 1 and t.stride(1) != 1)) for t in (x, x_rot)):
+        raise JanusError(f"{what}: x and x_rot are to be [{batch.total_q}, elements] of one type, elements adjacent")
+    xdt = _float_code(what, "x", given)
+    n = sum(int(t.shape[1]) for t in (x, x_rot) if t is not None)
+    if size is not None and int(size) != n:
+        raise JanusError(f"{what}: the rows have {n} elements, not {size}")
+    if x_rot is not None and (rotary is None or x_rot.shape[1] != rotary.dim):
+        raise JanusError(f"{what}: x_rot holds the elements that rotary turns")
+    odt = _dtype_code(out, None)
+    if out.dim() < 1 or out.shape[-1] < n or not out.is_contiguous() or out.dtype == torch.int16:
+        raise JanusError(f"{what}: out is to be contiguous rows of at least {n} elements, float32, bfloat16 or fp8")
+    num_rows = out.numel() // int(out.shape[-1])
+    if rows is not None:
+        _want(what, "rows", rows, torch.int64, batch.total_q)
+    elif num_rows < batch.total_ctx:
+        raise JanusError(f"{what}: {num_rows} rows for {batch.total_ctx} keys")
+    if out_scale is not None:
+        if odt != JANUS_FP8_E4M3:
+            raise JanusError(f"{what}: out_scale goes with fp8 rows")
+        if out_scale.dtype != torch.float32 or not out_scale.is_contiguous() or out_scale.numel() != num_rows:
+            raise JanusError(f"{what}: out_scale is to hold one float32 for each of {num_rows} rows")
+    if rotary is not None:
+        rotary._check(what, batch)
+    dev = _device(what, out, x, x_rot, rows, out_scale, batch.q_start, None if rotary is None else rotary.inv_freq)
+    if batch.total_q:
+        _launch(what, dev, stream, lib().janus_kv_append, batch.ref, None if rotary is None else rotary.ref, _ptr(x),
+                xdt, 0 if x is None else x.stride(0), _ptr(x_rot), 0 if x_rot is None else x_rot.stride(0), n,
+                _ptr(rows), num_rows, _ptr(out), odt, int(out.shape[-1]) * out.element_size(), _ptr(out_scale))
+    return out
+
+
+def prefix_attn(batch: Batch, q, k_pool, v_pool, page_table, page_size: int, prefix_len: int, scale: float,
+                k_row_stride: Optional[int] = None, v_row_stride: Optional[int] = None, dv: Optional[int] = None,
+                out_dtype: str = "bf16", want_lse: bool = False, out=None, lse=None, workspace=None, stream=None):
+    """janus_prefix_attn: dense causal attention of the appended tokens over all
+    cached ids, the first prefix_len of them common to the batch's sessions;
+    returns (out, lse or None).  q, pools, out and lse as for sparse_attn, workspace
+    as for sparse_attn_split."""
+    what = "janus_prefix_attn"
+    if q.dim() != 3 or q.shape[0] != batch.total_q or q.dtype != torch.bfloat16 or not q.is_contiguous():
+        raise JanusError(f"{what}: q is to be a contiguous bfloat16 [{batch.total_q}, heads, dims], not {tuple(q.shape)}")
+    Hq, dqk = int(q.shape[1]), int(q.shape[2])
+    krs = int(k_row_stride if k_row_stride is not None else k_pool.shape[-1])
+    vrs = int(v_row_stride if v_row_stride is not None else v_pool.shape[-1])
+    dv = int(dv if dv is not None else (v_pool.shape[-1] if v_pool is not k_pool else dqk))
+    if any(p.dtype != torch.bfloat16 for p in (k_pool, v_pool)) or out_dtype not in ("bf16", "f32"):
+        raise JanusError(f"{what}: bfloat16 pools and out_dtype bf16 or f32 expected")
+    _want(what, "page_table", page_table, torch.int32, batch.c.num_seqs, None)
+    odt = {"bf16": (JANUS_BF16, torch.bfloat16), "f32": (JANUS_F32, torch.float32)}[out_dtype]
+    if out is None:
+        out = torch.empty((batch.total_q, Hq, dv), dtype=odt[1], device=q.device)
+    _want(what, "out", out, odt[1], batch.total_q, Hq, dv)
+    if want_lse and lse is None:
+        lse = torch.empty((batch.total_q, Hq), dtype=torch.float32, device=q.device)
+    if lse is not None:
+        _want(what, "lse", lse, torch.float32, batch.total_q, Hq)
+    dev = _device(what, q, k_pool, v_pool, page_table, out, lse, workspace, batch.q_start)
+    if batch.total_q == 0:
+        return out, lse
+    args = (batch.ref, _ptr(q), Hq, dqk, dv, _ptr(k_pool), _ptr(v_pool), krs, vrs, _ptr(page_table),
+            _table(batch, page_table, page_size), int(page_size), int(prefix_len), float(scale), _ptr(out), odt[0],
+            _ptr(lse))
+    need = ctypes.c_size_t(0)
+    _launch(what, dev, stream, lib().janus_prefix_attn, *args, None, ctypes.byref(need))
+    if workspace is None:
+        workspace = torch.empty(max(int(need.value), 1), dtype=torch.uint8, device=q.device)
+    have = ctypes.c_size_t(workspace.numel() * workspace.element_size())
+    _launch(what, dev, stream, lib().janus_prefix_attn, *args, _ptr(workspace), ctypes.byref(have))
     return out, lse

@@ -164,4 +164,98 @@ constexpr bool mqa_shared(int64_t total_q, int64_t k)
     return k > 100 && one * (3400 + 12 * k) < four * (3800 + 49 * k);
 }
 
+// ---- shared-prefix attention: blocks of 128 rows and a range of keys ------------
+
+constexpr int PA_ROWS = 128;  // (token, head) rows of a block
+constexpr int PA_XCD = 8;
+constexpr int PA_CUS = 256;
+
+// First tile of session s's own rows, whose tokens start at q_start: each session has as
+// many tiles as its rows fill, or one more, and none needs the sessions before
+// its own.  (With 128 heads every token is a tile.)
+constexpr int prefix_tile_first(int q_start, int heads, int s)
+{
+    return (int)((int64_t)q_start * heads / PA_ROWS) + (heads % PA_ROWS != 0 ? s : 0);
+}
+
+struct PrefixPlan {
+    int rows;          // total_q * heads
+    int prefix;        // ids that rows of different sessions meet together
+    int chunk;         // keys of a block
+    int shared_tiles, shared_chunks;  // over the prefix
+    int own_tiles, own_chunks;        // over the ids behind it
+    int alike;         // own chunks that read the same pages in every session
+    int slots;         // ranges of a row
+    int64_t blocks;
+};
+
+constexpr PrefixPlan prefix_plan(int num_seqs, int total_q, int max_q, int max_ctx, int64_t total_ctx, int prefix_len,
+                                 int heads, bool mla)
+{
+    PrefixPlan p = {};
+    (void)max_q;
+    p.rows = total_q * heads;
+    const int full = (p.rows + PA_ROWS - 1) / PA_ROWS;  // tiles of all rows together
+    // tiles of the sessions apart, at the mean length
+    const int64_t each = ((int64_t)p.rows / num_seqs + PA_ROWS - 1) / PA_ROWS;
+    const int64_t apart = num_seqs * (each > 1 ? each : 1);
+    const bool share = prefix_len > 0 && (int64_t)full * 8 <= apart * 7;
+    p.prefix = share ? prefix_len : 0;
+    p.shared_tiles = share ? full : 0;
+    p.own_tiles = prefix_tile_first(total_q, heads, num_seqs);
+    const int own = max_ctx - p.prefix;
+    const int64_t mean = total_ctx / num_seqs > p.prefix ? total_ctx / num_seqs - p.prefix : 0;
+    const int span = own > p.prefix ? own : p.prefix;
+    const int tile = mla ? 32 : 64, resident = PA_CUS * (mla ? 1 : 2);
+    // a block's start, and moving a row's range out and in again, in keys
+    const int start = mla ? 128 : 256;
+    double best = -1.0;
+    for (int n = 1; n <= 256; n += 1 + n / 16) {
+        const int chunk = (span > n ? (span + n - 1) / n + tile - 1 : tile) / tile * tile;
+        const int sc = share ? (prefix_len + chunk - 1) / chunk : 0, oc = own > 0 ? (own + chunk - 1) / chunk : 1;
+        const int64_t work = (int64_t)p.shared_tiles * sc + apart * ((mean + chunk - 1) / chunk);
+        const int64_t rounds = (work + resident - 1) / resident;
+        const double cost = (double)rounds * (chunk + start) +
+                            (sc + oc > 1 ? (double)(sc + oc) * p.rows * (mla ? 0.02 : 0.01) + start : 0.0);
+        if (best < 0.0 || cost < best) {
+            best = cost;
+            p.chunk = chunk;
+            p.shared_chunks = sc;
+            p.own_chunks = oc;
+        }
+        if (chunk == tile)
+            break;
+    }
+    p.alike = share ? 0 : prefix_len / p.chunk;
+    p.slots = p.shared_chunks + p.own_chunks;
+    p.blocks = (int64_t)p.shared_tiles * p.shared_chunks + (int64_t)p.own_tiles * p.own_chunks;
+    return p;
+}
+
+// Block blk of a plan.  Blocks that read the same keys are neighbours in the numbering,
+// and blocks of one XCD (blk % 8) have consecutive numbers: the keys come into one L2.
+struct PrefixBlock {
+    bool shared;
+    int tile, chunk, slot;
+};
+constexpr int64_t prefix_xcd(int64_t blk, int64_t n)
+{
+    const int64_t x = blk % PA_XCD, per = n / PA_XCD, more = n % PA_XCD;
+    return x * per + (x < more ? x : more) + blk / PA_XCD;
+}
+constexpr PrefixBlock prefix_block(const PrefixPlan &p, int64_t blk)
+{
+    const int64_t together = (int64_t)p.shared_tiles * p.shared_chunks;
+    if (blk < together) {
+        const int64_t id = prefix_xcd(blk, together);
+        const int c = (int)(id / p.shared_tiles);
+        return {true, (int)(id % p.shared_tiles), c, c};
+    }
+    blk -= together;
+    const int64_t alike = (int64_t)p.own_tiles * p.alike;
+    const int64_t id = blk < alike ? prefix_xcd(blk, alike) : blk;
+    const int c = (int)(id / p.own_tiles);
+    return {false, (int)(id % p.own_tiles), c, p.shared_chunks + c};
+}
+
 } // namespace janus

@@ -1,0 +1,507 @@
+// Rotary positions, and the rows of the caches.
+//
+// A rotated head takes its pairs (x_a, x_b) to
+//
+//   (m (x_a cos t - x_b sin t), m (x_b cos t + x_a sin t)),  t = position * inv_freq[pair]
+//
+// (t negated for the transpose).  t is reduced to a fraction of a turn in 64
+// bits, where far positions lose nothing, and its sine and cosine are taken of
+// that fraction in 32.  They are worked out once per token and pair, into LDS,
+// and used by all heads.
+//
+// One kernel does queries (many heads a token, written in place or apart) and
+// cache rows (one head a token, scattered through a slot map), to fp32, bf16 or
+// fp8 with one scale per token.  A token is LPR lanes (16, 64 or 256, by the
+// length of its row): an fp8 row's largest value is then a reduction over
+// those lanes, and short rows share a block.  A lane's unit is two groups of V
+// elements: the two halves of V pairs that lie apart, or 2 V neighbours.  Loads go out before the
+// angles are worked out.  Bound by the bytes read and written.
+#include "janus_device.hpp"
+#include "janus_host.hpp"
+
+#include <math.h>
+#include <type_traits>
+
+namespace janus {
+
+constexpr int ROPE_THREADS = 256;
+constexpr int ROPE_UPT = 2;          // units in a lane's registers
+constexpr int ROPE_MAX_DIM = 1024;   // sines and cosines of a block fit in LDS
+constexpr float FP8_LARGEST = 448.f;
+constexpr float AMAX_FLOOR = 1e-12f;  // an all-zero row's scale stays positive
+
+struct RopeArgs {
+    const int32_t *q_start, *ctx_start, *hist_len;
+    int num_seqs, es, total_q;
+    const void *x;               // plain elements (all of them where xr == nullptr)
+    const void *xr;              // rotated elements, or nullptr
+    int64_t x_rs, x_hs, xr_rs;   // strides in elements
+    int heads, size, off, dim;   // a head's elements, and the rotated ones among them
+    int halves, inverse;         // pairs (j, j + dim/2); transpose
+    float mag;
+    const double *inv_freq;
+    const int32_t *positions;
+    uint8_t *out;
+    int64_t o_rs, o_hs;          // bytes
+    int plain_units;             // units a head of the elements that are only copied (0: in place)
+    int scatter;                 // cache rows: to `rows`, or by context where it is null
+    const int64_t *rows;
+    int64_t num_rows;
+    float *scale;                // fp8: one per output row; null: in the row, behind its elements
+};
+
+// Session of `row`, found by LPR lanes together (64 at most).
+template <int LPR>
+JANUS_DEV int session_of_row_lanes(const int32_t *q_start, int num_seqs, int row)
+{
+    constexpr int K = LPR < kWave ? LPR : kWave;
+    const int lane = threadIdx.x & 63, in = lane & (K - 1);
+    int lo = 0, hi = num_seqs;  // the session is in [lo, hi)
+    while (__ballot(hi - lo > 1) != 0) {
+        const int step = max(1, (hi - lo + K - 1) / K);
+        const int s = lo + in * step;
+        uint64_t below = __ballot(s < hi && q_start[s] <= row);
+        if constexpr (K < kWave)
+            below = (below >> (lane & ~(K - 1))) & ((1ull << K) - 1);
+        lo += max(__popcll(below) - 1, 0) * step;
+        hi = min(hi, lo + step);
+    }
+    return lo;
+}
+
+template <class T, int V>
+JANUS_DEV void load_group(const T *p, float (&v)[V])
+{
+    if constexpr (V == 1) {
+        if constexpr (std::is_same<T, float>::value)
+            v[0] = *p;
+        else
+            v[0] = bf16_to_f32(*p);
+    } else if constexpr (std::is_same<T, float>::value) {
+        const v4f a = ((const v4f *)p)[0], b = ((const v4f *)p)[1];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[e] = a[e];
+            v[4 + e] = b[e];
+        }
+    } else {
+        const v4i a = *(const v4i *)p;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[2 * e] = __uint_as_float((uint32_t)a[e] << 16);
+            v[2 * e + 1] = __uint_as_float((uint32_t)a[e] & 0xffff0000u);
+        }
+    }
+}
+
+// To the nearest bf16, ties to even (NaN stays NaN).
+JANUS_DEV uint32_t bf16_pair(float a, float b)
+{
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v2f{a, b}, v2bf));
+}
+// To the nearest e4m3, ties to even; beyond the largest value: that value (NaN stays NaN).
+JANUS_DEV uint32_t fp8_quad(float a, float b, float c, float d)
+{
+    auto fit = [](float x) { return fabsf(x) > FP8_LARGEST ? copysignf(FP8_LARGEST, x) : x; };
+    v2s w = {0, 0};
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, fit(a), fit(b), 1.0f, false);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, fit(c), fit(d), 1.0f, true);
+    return __builtin_bit_cast(uint32_t, w);
+}
+
+template <int DT, int V>
+JANUS_DEV void store_group(uint8_t *p, const float (&v)[V], float inv)
+{
+    if constexpr (DT == JANUS_F32) {
+        if constexpr (V == 1) {
+            *(float *)p = v[0];
+        } else {
+            ((v4f *)p)[0] = v4f{v[0], v[1], v[2], v[3]};
+            ((v4f *)p)[1] = v4f{v[4], v[5], v[6], v[7]};
+        }
+    } else if constexpr (DT == JANUS_BF16) {
+        if constexpr (V == 1)
+            *(uint16_t *)p = (uint16_t)bf16_pair(v[0], 0.f);
+        else
+            *(v4i *)p = v4i{(int)bf16_pair(v[0], v[1]), (int)bf16_pair(v[2], v[3]), (int)bf16_pair(v[4], v[5]),
+                            (int)bf16_pair(v[6], v[7])};
+    } else {
+        if constexpr (V == 1)
+            *p = (uint8_t)fp8_quad(v[0] * inv, 0.f, 0.f, 0.f);
+        else
+            *(v2i *)p = v2i{(int)fp8_quad(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv),
+                            (int)fp8_quad(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv)};
+    }
+}
+
+// Where a unit lies: its head, the first elements of its two groups in the
+// head (b < 0: one group), and its first pair (-1: not rotated).
+struct Unit {
+    int head, a, b, pair;
+};
+template <int V>
+JANUS_DEV Unit unit_at(const RopeArgs &g, int u)
+{
+    const int turned = g.dim / (2 * V), per = turned + g.plain_units;
+    Unit at;
+    at.head = u / per;
+    const int r = u - at.head * per;
+    if (r < turned) {
+        at.pair = r * V;
+        at.a = g.off + (g.halves ? r * V : 2 * r * V);
+        at.b = at.a + (g.halves ? g.dim / 2 : V);
+    } else {
+        const int e = 2 * V * (r - turned);  // among the plain elements
+        at.pair = -1;
+        at.a = e < g.off ? e : e + g.dim;
+        at.b = e + V < g.off ? e + V : e + V + g.dim;
+        if (at.b >= g.size)
+            at.b = -1;
+    }
+    return at;
+}
+
+template <class T, int DT, int V, int LPR>
+__global__ __launch_bounds__(ROPE_THREADS) void rope_rows(RopeArgs g)
+{
+    extern __shared__ float2 turn[];  // [rows of the block][dim / 2]: cosine, sine
+    __shared__ float red[ROPE_THREADS / kWave];
+    __shared__ int sPos[ROPE_THREADS / LPR];
+    constexpr int ROWS = ROPE_THREADS / LPR;
+    constexpr bool FP8 = DT == JANUS_FP8_E4M3;
+    const int tid = threadIdx.x, lane = tid % LPR, mine = tid / LPR;
+    const int row = blockIdx.x * ROWS + mine;
+    const bool live = row < g.total_q;
+    const int pairs = g.dim / 2;
+    const int units = g.heads * (g.dim / (2 * V) + g.plain_units);
+    // fp8 rows: all units of the token, LPR * ROPE_UPT at a time; others: the block's share of them
+    const int u0 = FP8 ? 0 : blockIdx.y * LPR * ROPE_UPT;
+
+    float va[ROPE_UPT][V], vb[ROPE_UPT][V];
+    auto load = [&](int first) {
+#pragma unroll
+        for (int k = 0; k < ROPE_UPT; ++k) {
+            const int u = first + k * LPR + lane;
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                va[k][e] = vb[k][e] = 0.f;
+            if (!live || u >= units)
+                continue;
+            const Unit at = unit_at<V>(g, u);
+            if (at.pair >= 0 && g.xr) {
+                const T *p = (const T *)g.xr + (int64_t)row * g.xr_rs - g.off;
+                load_group<T, V>(p + at.a, va[k]);
+                load_group<T, V>(p + at.b, vb[k]);
+            } else {
+                const T *p = (const T *)g.x + (int64_t)row * g.x_rs + (int64_t)at.head * g.x_hs;
+                const int skip = g.xr ? g.dim : 0;  // the rotated elements are elsewhere
+                load_group<T, V>(p + (at.a < g.off ? at.a : at.a - skip), va[k]);
+                if (at.b >= 0)
+                    load_group<T, V>(p + (at.b < g.off ? at.b : at.b - skip), vb[k]);
+            }
+        }
+    };
+    load(u0);
+
+    // the token's session, position and output row
+    int64_t to = row;
+    bool store = live && row < g.q_start[g.num_seqs];
+    {
+        const int b = session_of_row_lanes<LPR>(g.q_start, g.num_seqs, live ? row : 0);
+        const int tokens = g.hist_len[b] + row - g.q_start[b] + 1;
+        if (lane == 0)
+            sPos[mine] = live && g.positions ? g.positions[row] : tokens - 1;
+        if (g.scatter) {
+            if (g.rows) {
+                to = live ? g.rows[row] : -1;
+            } else {
+                to = (int64_t)g.ctx_start[b] + entries_of(tokens, g.es) - 1;
+                store = store && (tokens & ((1 << g.es) - 1)) == 0;
+            }
+            store = store && to >= 0 && to < g.num_rows;
+        }
+    }
+    __syncthreads();
+    for (int i = tid; i < ROWS * pairs; i += ROPE_THREADS) {
+        const int r = i / pairs, p = i - r * pairs;
+        double t = (double)sPos[r] * g.inv_freq[p] * 0.15915494309189533577;  // turns
+        t -= rint(t);
+        float s, c;
+        sincospif(2.f * (float)t, &s, &c);
+        turn[i] = float2{c * g.mag, (g.inverse ? -s : s) * g.mag};
+    }
+    __syncthreads();
+    auto rotate = [&](int first) {
+#pragma unroll
+        for (int k = 0; k < ROPE_UPT; ++k) {
+            const int u = first + k * LPR + lane;
+            if (u >= units)
+                continue;
+            const Unit at = unit_at<V>(g, u);
+            if (at.pair < 0)
+                continue;
+            const float2 *t = turn + mine * pairs + at.pair;
+            if (g.halves || V == 1) {
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float a = va[k][e], b = vb[k][e];
+                    va[k][e] = a * t[e].x - b * t[e].y;
+                    vb[k][e] = b * t[e].x + a * t[e].y;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < V; e += 2) {
+                    const float a = va[k][e], b = va[k][e + 1], c = vb[k][e], d = vb[k][e + 1];
+                    const float2 ta = t[e / 2], tb = t[(V + e) / 2];
+                    va[k][e] = a * ta.x - b * ta.y;
+                    va[k][e + 1] = b * ta.x + a * ta.y;
+                    vb[k][e] = c * tb.x - d * tb.y;
+                    vb[k][e + 1] = d * tb.x + c * tb.y;
+                }
+            }
+        }
+    };
+    constexpr int BYTES = FP8 ? 1 : DT == JANUS_BF16 ? 2 : 4;
+    auto put = [&](int first, float inv) {
+#pragma unroll
+        for (int k = 0; k < ROPE_UPT; ++k) {
+            const int u = first + k * LPR + lane;
+            if (u >= units || !store)
+                continue;
+            const Unit at = unit_at<V>(g, u);
+            uint8_t *p = g.out + to * g.o_rs + (int64_t)at.head * g.o_hs;
+            store_group<DT, V>(p + (int64_t)at.a * BYTES, va[k], inv);
+            if (at.b >= 0)
+                store_group<DT, V>(p + (int64_t)at.b * BYTES, vb[k], inv);
+        }
+    };
+    rotate(u0);
+    if constexpr (!FP8) {
+        put(u0, 1.f);
+    } else {
+        // largest finite magnitude of the token
+        float top = 0.f;
+        auto tops = [&]() {
+#pragma unroll
+            for (int k = 0; k < ROPE_UPT; ++k)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float a = fabsf(va[k][e]), b = fabsf(vb[k][e]);
+                    top = fmaxf(top, a < INFINITY ? a : 0.f);
+                    top = fmaxf(top, b < INFINITY ? b : 0.f);
+                }
+        };
+        tops();
+        const bool again = units > LPR * ROPE_UPT;
+        for (int u = LPR * ROPE_UPT; u < units; u += LPR * ROPE_UPT) {
+            load(u);
+            rotate(u);
+            tops();
+        }
+#pragma unroll
+        for (int o = 1; o < (LPR < kWave ? LPR : kWave); o <<= 1)
+            top = fmaxf(top, __shfl_xor(top, o));
+        if constexpr (LPR > kWave) {
+            if ((tid & 63) == 0)
+                red[tid >> 6] = top;
+            __syncthreads();
+            top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+        }
+        const float scale = fmaxf(top, AMAX_FLOOR) / FP8_LARGEST, inv = 1.f / scale;
+        if (again) {
+            // a row longer than the lanes' registers is read again
+            for (int u = 0; u < units; u += LPR * ROPE_UPT) {
+                load(u);
+                rotate(u);
+                put(u, inv);
+            }
+        } else {
+            put(0, inv);
+        }
+        if (lane == 0 && store) {
+            if (g.scale)
+                g.scale[to] = scale;
+            else
+                *(float *)(g.out + to * g.o_rs + g.size) = scale;
+        }
+    }
+}
+
+template <class T, int DT, int V>
+static void launch_rope_rows(const RopeArgs &g, hipStream_t st)
+{
+    const int units = g.heads * (g.dim / (2 * V) + g.plain_units);
+    const int most = DT == JANUS_FP8_E4M3 ? 1 : 65535;
+    auto go = [&](auto lanes) {
+        constexpr int LPR = decltype(lanes)::value;
+        const int rows = ROPE_THREADS / LPR;
+        hipLaunchKernelGGL((rope_rows<T, DT, V, LPR>),
+                           dim3(ceil_div(g.total_q, rows),
+                                most == 1 ? 1 : ceil_div(units, LPR * ROPE_UPT)),
+                           dim3(ROPE_THREADS), (size_t)rows * (g.dim / 2) * sizeof(float2), st, g);
+    };
+    if (units <= 16 * ROPE_UPT)
+        go(std::integral_constant<int, 16>{});
+    else if (units <= 64 * ROPE_UPT)
+        go(std::integral_constant<int, 64>{});
+    else
+        go(std::integral_constant<int, 256>{});
+}
+
+template <class T>
+static int launch_rope(RopeArgs g, int x_dt, int out_dt, bool in_place, hipStream_t st)
+{
+    // Groups of eight where every one of them is 16 bytes (8 in fp8 rows) at an
+    // address of that alignment, else single elements.
+    const int64_t in = x_dt == JANUS_F32 ? 4 : 8, align = out_dt == JANUS_FP8_E4M3 ? 8 : 16;
+    auto at = [](const void *p, int64_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; };
+    const bool wide = g.dim % 16 == 0 && g.off % 8 == 0 && g.size % 8 == 0 && at(g.x, 16) && at(g.xr, 16) &&
+                      at(g.out, align) && g.x_rs % in == 0 && g.x_hs % in == 0 && g.xr_rs % in == 0 &&
+                      g.o_rs % align == 0 && g.o_hs % align == 0;
+    const int plain = in_place ? 0 : g.size - g.dim;
+    auto go = [&](auto dt) {
+        constexpr int DT = decltype(dt)::value;
+        if (wide) {
+            g.plain_units = (plain + 15) / 16;
+            launch_rope_rows<T, DT, 8>(g, st);
+        } else {
+            g.plain_units = (plain + 1) / 2;
+            launch_rope_rows<T, DT, 1>(g, st);
+        }
+    };
+    if (out_dt == JANUS_F32)
+        go(std::integral_constant<int, JANUS_F32>{});
+    else if (out_dt == JANUS_BF16)
+        go(std::integral_constant<int, JANUS_BF16>{});
+    else
+        go(std::integral_constant<int, JANUS_FP8_E4M3>{});
+    return launch_status();
+}
+
+static bool rotary_ok(const janus_rotary *r, int size)
+{
+    return r && r->dim >= 2 && r->dim % 2 == 0 && r->offset >= 0 && r->offset <= size - r->dim && r->inv_freq &&
+           (r->layout == JANUS_ROTARY_HALVES || r->layout == JANUS_ROTARY_INTERLEAVED);
+}
+
+static RopeArgs rope_args(const janus_batch *b, const janus_rotary *r)
+{
+    RopeArgs g = {};
+    g.q_start = b->q_start;
+    g.ctx_start = b->ctx_start;
+    g.hist_len = b->hist_len;
+    g.num_seqs = b->num_seqs;
+    g.es = b->entry_shift;
+    g.total_q = b->total_q;
+    if (r) {
+        g.off = r->offset;
+        g.dim = r->dim;
+        g.halves = r->layout == JANUS_ROTARY_HALVES;
+        g.inverse = r->inverse != 0;
+        g.mag = r->magnitude;
+        g.inv_freq = r->inv_freq;
+        g.positions = r->positions;
+    }
+    return g;
+}
+
+}  // namespace janus
+
+using namespace janus;
+
+extern "C" int janus_rope(const janus_batch *b, const janus_rotary *r, const void *x, janus_dtype x_dt,
+                          int64_t x_row_stride, int64_t x_head_stride, int heads, int size, void *out,
+                          janus_dtype out_dt, int64_t out_row_stride, int64_t out_head_stride, float *out_scale,
+                          void *stream)
+{
+    if (!batch_ok(b) || !x || !out || heads < 1 || size < 1 || !rotary_ok(r, size) || !dtype_ok(x_dt) ||
+        !dtype_ok(out_dt) || x_row_stride < 0 || x_head_stride < 0 || out_row_stride < 0 || out_head_stride < 0)
+        return JANUS_ERR_INVALID_ARG;
+    const bool fp8 = out_dt == JANUS_FP8_E4M3;
+    if (fp8 != (out_scale != nullptr))
+        return JANUS_ERR_INVALID_ARG;
+    const bool in_place = out == x;
+    if (in_place && (x_dt != out_dt || x_row_stride != out_row_stride || x_head_stride != out_head_stride))
+        return JANUS_ERR_INVALID_ARG;
+    if (x_dt == JANUS_FP8_E4M3 || r->dim > ROPE_MAX_DIM || (int64_t)heads * size > (1 << 24))
+        return JANUS_ERR_UNSUPPORTED;
+    if (b->total_q == 0)
+        return JANUS_OK;
+    const int64_t ob = out_dt == JANUS_F32 ? 4 : out_dt == JANUS_BF16 ? 2 : 1;
+    RopeArgs g = rope_args(b, r);
+    g.x = x;
+    g.x_rs = x_row_stride;
+    g.x_hs = x_head_stride;
+    g.heads = heads;
+    g.size = size;
+    g.out = (uint8_t *)out;
+    g.o_rs = out_row_stride * ob;
+    g.o_hs = out_head_stride * ob;
+    g.scale = out_scale;
+    return x_dt == JANUS_F32 ? launch_rope<float>(g, x_dt, out_dt, in_place, as_stream(stream))
+                             : launch_rope<uint16_t>(g, x_dt, out_dt, in_place, as_stream(stream));
+}
+
+extern "C" int janus_kv_append(const janus_batch *b, const janus_rotary *r, const void *x, janus_dtype x_dt,
+                               int64_t x_row_stride, const void *x_rot, int64_t x_rot_stride, int size,
+                               const int64_t *rows, int64_t num_rows, void *out, janus_dtype out_dt,
+                               int64_t out_row_bytes, float *out_scale, void *stream)
+{
+    if (!batch_ok(b) || !out || size < 1 || num_rows < 0 || !dtype_ok(x_dt) || !dtype_ok(out_dt) ||
+        x_row_stride < 0 || x_rot_stride < 0 || (r && !rotary_ok(r, size)) || (x_rot && !r) ||
+        (!x && !(x_rot && r->dim == size)) || (!rows && !b->ctx_start))
+        return JANUS_ERR_INVALID_ARG;
+    const int64_t ob = out_dt == JANUS_F32 ? 4 : out_dt == JANUS_BF16 ? 2 : 1;
+    const bool fp8 = out_dt == JANUS_FP8_E4M3, inlined = fp8 && !out_scale;
+    if (out_row_bytes < size * ob + (inlined ? 4 : 0) || out_row_bytes % ob != 0 || (out_scale && !fp8))
+        return JANUS_ERR_INVALID_ARG;
+    if (x_dt == JANUS_FP8_E4M3 || (r && r->dim > ROPE_MAX_DIM) || size > (1 << 24))
+        return JANUS_ERR_UNSUPPORTED;
+    // the scale in the row is one aligned word
+    if (inlined && (size % 4 != 0 || out_row_bytes % 4 != 0 || (reinterpret_cast<uintptr_t>(out) & 3) != 0))
+        return JANUS_ERR_UNSUPPORTED;
+    if (b->total_q == 0 || num_rows == 0)
+        return JANUS_OK;
+    RopeArgs g = rope_args(b, r);
+    g.x = x;
+    g.xr = x_rot;
+    g.x_rs = x_row_stride;
+    g.xr_rs = x_rot_stride;
+    g.heads = 1;
+    g.size = size;
+    g.out = (uint8_t *)out;
+    g.o_rs = out_row_bytes;
+    g.scatter = 1;
+    g.rows = rows;
+    g.num_rows = num_rows;
+    g.scale = out_scale;
+    return x_dt == JANUS_F32 ? launch_rope<float>(g, x_dt, out_dt, false, as_stream(stream))
+                             : launch_rope<uint16_t>(g, x_dt, out_dt, false, as_stream(stream));
+}
+
+extern "C" int janus_rotary_frequencies(int dim, double base, double factor, int scaling, int original_ctx,
+                                        double beta_fast, double beta_slow, double *inv_freq, float *magnitude)
+{
+    if (dim < 2 || dim % 2 != 0 || !(base > 1.0) || !inv_freq || !magnitude || !(factor >= 1.0) ||
+        scaling < JANUS_SCALING_NONE || scaling > JANUS_SCALING_YARN ||
+        (scaling == JANUS_SCALING_YARN && (original_ctx < 1 || !(beta_slow > 0.0) || !(beta_fast > beta_slow))))
+        return JANUS_ERR_INVALID_ARG;
+    // the pair whose wave makes `turns` turns over the original context
+    auto pair_of = [&](double turns) { return dim * log(original_ctx / (2.0 * M_PI * turns)) / (2.0 * log(base)); };
+    double low = 0.0, high = 0.0;
+    if (scaling == JANUS_SCALING_YARN) {
+        low = fmax(floor(pair_of(beta_fast)), 0.0);
+        high = fmin(ceil(pair_of(beta_slow)), dim - 1.0);
+    }
+    for (int j = 0; j < dim / 2; ++j) {
+        const double f = pow(base, -2.0 * j / dim);
+        double stretched = 0.0;  // share of the stretched frequency
+        if (scaling == JANUS_SCALING_LINEAR)
+            stretched = 1.0;
+        else if (scaling == JANUS_SCALING_YARN)
+            stretched = fmin(fmax((j - low) / fmax(high - low, 1e-3), 0.0), 1.0);
+        inv_freq[j] = f * (1.0 - stretched) + f / factor * stretched;
+    }
+    *magnitude = scaling == JANUS_SCALING_YARN ? (float)(0.1 * log(factor) + 1.0) : 1.0f;
+    return JANUS_OK;
+}

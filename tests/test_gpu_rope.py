@@ -1,0 +1,255 @@
+"""janus_rope and janus_kv_append against the rotation's formula in 64 bits.
+
+Tolerances.  The fraction of a turn is rounded to fp32 (2^-26 turns, under 2^-23
+rad), its sine and cosine are within 2 ulp (2^-23), and the two products and their sum
+round three times: a result is within 2^-21 (|x_a| + |x_b|) * magnitude of the exact one.  A
+rounding to bf16 adds 2^-8 of the value, one to e4m3 2^-4 of it, or half of the
+smallest step, 2^-10 of the scale.  A largest value of a row is off by 2^-21 of |x_a| + |x_b| <= 2 of itself:
+2^-20, and with the division 2^-19."""
+import numpy as np
+import pytest
+import torch
+
+from plain import bf16, positions, rotate
+
+pytestmark = pytest.mark.gpu
+janus = pytest.importorskip("paper_2609_36938_amd")
+
+F32 = 2.0 ** -21
+
+
+def _freq(dim, scaling=None):
+    return janus.rotary_frequencies(dim, 10000.0, scaling, 40.0 if scaling else 1.0, 4096)
+
+
+def _inputs(total, heads, size, dt, seed):
+    x = np.random.default_rng(seed).standard_normal((total, heads, size)).astype(np.float32)
+    t = torch.from_numpy(x).cuda().to(torch.bfloat16 if dt == "bf16" else torch.float32)
+    return t, t.double().cpu().numpy()
+
+
+def _close(got, want, mass, dt):
+    tol = F32 * mass + (2.0 ** -8 * np.abs(want) if dt == "bf16" else 0)
+    err = np.abs(got.double().cpu().numpy() - want)
+    assert (err <= tol).all(), (err - tol).max()
+
+
+def _fp8(x):
+    return x.view(torch.float8_e4m3fn).double().cpu().numpy()
+
+
+def _close_fp8(codes, scale, y):
+    """codes [rows, n] and scale [rows] against the exact rows y."""
+    amax = np.maximum(np.abs(y).max(1), 1e-12)
+    s = scale.double().cpu().numpy()
+    assert (np.abs(s - amax / 448) <= 2.0 ** -19 * amax / 448).all()
+    held = codes * s[:, None]
+    tol = 2.0 ** -4 * np.abs(y) + (2.0 ** -10 * amax / 448 + 2.0 ** -18 * amax)[:, None]
+    assert (np.abs(held - y) <= tol).all()
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("heads,size,dim,off,hist,new", [
+    (1, 64, 64, 0, [5], [1]),
+    (8, 128, 128, 0, [0, 131072, 7], [3, 0, 41]),
+    (64, 128, 64, 0, [1000003], [9]),
+    (3, 576, 64, 512, [100, 20], [30, 77]),
+    (5, 30, 10, 3, [9], [65]),                  # nothing aligned
+    (1, 2, 2, 0, [0], [300]),
+    (2, 1040, 1024, 8, [50], [7]),
+    (128, 64, 48, 16, [70] * 70, [1] * 70),
+    (300, 8, 6, 1, [3], [2]),
+])
+def test_rotation(heads, size, dim, off, hist, new, layout, dt):
+    freq, _ = _freq(dim)
+    x, xd = _inputs(sum(new), heads, size, dt, dim)
+    bt = janus.Batch(hist, new)
+    want, mass = rotate(xd, positions(hist, new), freq, off, layout)
+    rot = janus.Rotary(dim, off, layout)
+    print("rope", heads, size, dim, off, layout, dt, flush=True)
+    out, scale = janus.rope(bt, rot, x)
+    assert scale is None
+    _close(out, want, mass, dt)
+    other = "f32" if dt == "bf16" else "bf16"
+    _close(janus.rope(bt, rot, x, out_dtype=other)[0], want, mass, other)
+    janus.rope(bt, rot, x, out=x)               # in place: the same bits
+    assert torch.equal(x, out)
+
+
+@pytest.mark.parametrize("scaling", ["linear", "yarn"])
+def test_scaled_positions_and_strides(scaling):
+    """The rotated tail of a projection's heads into the tail of the absorbed queries, with given positions."""
+    freq, mag = _freq(64, scaling)
+    T, H = 37, 16
+    pos = np.random.default_rng(3).integers(0, 1 << 20, T).astype(np.int32)
+    x, xd = _inputs(T, H, 192, "bf16", 4)
+    q = torch.full((T, H, 576), 7.0, dtype=torch.bfloat16, device="cuda")
+    rot = janus.Rotary(64, layout="interleaved", inv_freq=torch.from_numpy(freq).cuda(), mscale=mag,
+                       positions=torch.from_numpy(pos).cuda())
+    janus.rope(janus.Batch([0], [T]), rot, x[..., 128:], out=q[..., 512:])
+    want, mass = rotate(xd[..., 128:], pos, freq, 0, "interleaved", np.float32(mag))
+    _close(q[..., 512:], want, mass, "bf16")
+    assert (q[..., :512] == 7).all()
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_gradient(layout):
+    """The transpose against the formula's and against differences of the forward call."""
+    T, H, D = 11, 4, 128
+    x, _ = _inputs(T, H, D, "f32", 1)
+    gy, gd = _inputs(T, H, D, "f32", 2)
+    bt = janus.Batch([40000], [T])
+    rot = janus.Rotary(96, 16, layout, scaling="yarn", factor=8.0, original_ctx=2048)
+    gx = janus.rope(bt, rot.inverted(), gy)[0]
+    freq, mag = janus.rotary_frequencies(96, 10000.0, "yarn", 8.0, 2048)
+    want, mass = rotate(gd, positions([40000], [T]), freq, 16, layout, np.float32(mag), inverse=True)
+    _close(gx, want, mass, "f32")
+    # the map is linear: a difference in the direction v is the map of v; <J v, gy> = <v, gx>
+    v, vd = _inputs(T, H, D, "f32", 5)
+    eps = 0.5
+    up, down = (janus.rope(bt, rot, x + s * v)[0].double().cpu().numpy() for s in (eps, -eps))
+    left = ((up - down) / (2 * eps) * gd).sum((1, 2))
+    right = (vd * gx.double().cpu().numpy()).sum((1, 2))
+    # each of the T sums has H D terms, each off by 2^-21 * 2 mag of inputs under 5 in size, on both sides
+    assert (np.abs(left - right) <= H * D * 3 * F32 * 2 * mag * 5 * 5).all()
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,size,dim,off", [(64, 128, 64, 0), (1, 128, 64, 64), (4, 64, 64, 0), (3, 30, 10, 2),
+                                                (128, 576, 64, 512)])
+def test_fp8_queries(heads, size, dim, off, dt):
+    hist, new = [100, 0, 70000], [5, 20, 1]
+    x, xd = _inputs(26, heads, size, dt, 9)
+    x[3] = 0
+    xd[3] = 0
+    want = rotate(xd, positions(hist, new), _freq(dim)[0], off, "half")[0]
+    out, scale = janus.rope(janus.Batch(hist, new), janus.Rotary(dim, off), x, out_dtype="fp8")
+    _close_fp8(_fp8(out).reshape(26, -1), scale, want.reshape(26, -1))
+
+
+def test_fp8_of_values_that_are_not_finite():
+    """An infinity becomes the largest value, NaN stays NaN, and neither moves the scale."""
+    x, xd = _inputs(3, 2, 32, "f32", 1)
+    x[1, 0, 20], x[1, 1, 21], x[1, 0, 22] = float("inf"), float("nan"), float("-inf")
+    xd[1, 0, [20, 22]] = xd[1, 1, 21] = 0
+    out, scale = janus.rope(janus.Batch([0], [3]), janus.Rotary(16), x, out_dtype="fp8")
+    got = _fp8(out)
+    assert got[1, 0, 20] == 448 and got[1, 0, 22] == -448 and np.isnan(got[1, 1, 21])
+    got[1, 0, [20, 22]] = got[1, 1, 21] = 0
+    _close_fp8(got.reshape(3, -1), scale, rotate(xd, np.arange(3), _freq(16)[0], 0, "half")[0].reshape(3, -1))
+
+
+def test_rows_behind_the_last_session_stay():
+    x, xd = _inputs(70, 2, 64, "bf16", 3)
+    bt = janus.Batch([5], [9])
+    bt.total_q = bt.c.total_q = 70
+    out = torch.full_like(x, 3.0)
+    janus.rope(bt, janus.Rotary(64), x, out=out)
+    want, mass = rotate(xd[:9], positions([5], [9]), _freq(64)[0], 0, "half")
+    _close(out[:9], want, mass, "bf16")
+    assert (out[9:] == 3).all()
+
+
+# ---- cache rows ------------------------------------------------------------------
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["bf16", "f32", "inline", "scales"])
+@pytest.mark.parametrize("size,dim,off,width,split", [(576, 64, 512, 592, True), (128, 64, 0, 132, False),
+                                                      (36, 10, 3, 41, True), (128, 0, 0, 128, False),
+                                                      (64, 64, 0, 80, True)])
+def test_append(size, dim, off, width, split, kind, dt):
+    hist, new = [700, 0, 131000], [40, 1, 29]
+    T, R = 70, 200
+    rng = np.random.default_rng(size)
+    x, xd = _inputs(T, 1, size, dt, 6)
+    rows = rng.permutation(R)[:T].astype(np.int64)
+    rows[[3, 60]] = [-1, R]                      # nothing to write
+    pos = positions(hist, new)
+    y, mass = rotate(xd, pos, _freq(dim)[0] if dim else np.zeros(0), off, "interleaved")
+    y, mass = y[:, 0], mass[:, 0]
+    rot = janus.Rotary(dim, off, "interleaved") if dim else None
+    plain, part = x[:, 0], None
+    if split:
+        part = torch.cat([x[:, 0, off:off + dim], x[:, 0, :3]], 1)[:, :dim]  # a view with a longer stride
+        plain = torch.cat([x[:, 0, :off], x[:, 0, off + dim:]], 1) if size > dim else None
+    bt, rd = janus.Batch(hist, new), torch.from_numpy(rows).cuda()
+    kept = (rows >= 0) & (rows < R)
+    print("append", size, dim, kind, dt, flush=True)
+    if kind in ("bf16", "f32"):
+        pool = torch.full((R, width), 5.0, device="cuda").to(torch.bfloat16 if kind == "bf16" else torch.float32)
+        janus.kv_append(bt, plain, pool, rot, part, rd)
+        _close(pool[rows[kept], :size], y[kept], mass[kept], kind)
+        pool[rows[kept], :size] = 5
+        assert (pool == 5).all()
+        return
+    width = -(-width // 4) * 4 if kind == "inline" else width
+    pool = torch.full((R, width), 9, dtype=torch.uint8, device="cuda")
+    if kind == "inline":
+        if width < size + 4:
+            width = size + 4
+            pool = torch.full((R, width), 9, dtype=torch.uint8, device="cuda")
+        janus.kv_append(bt, plain, pool, rot, part, rd)
+        scale = pool[:, size:size + 4].contiguous().view(torch.float32)[:, 0]
+        end = size + 4
+    else:
+        scale = torch.full((R,), -1.0, device="cuda")
+        janus.kv_append(bt, plain, pool, rot, part, rd, out_scale=scale)
+        end = size
+        left = np.setdiff1d(np.arange(R), rows[kept])
+        assert (scale[left] == -1).all()
+    _close_fp8(_fp8(pool[:, :size].contiguous())[rows[kept]], scale[rows[kept]], y[kept])
+    pool[rows[kept], :end] = 9
+    assert (pool == 9).all()
+
+
+@pytest.mark.parametrize("es", [0, 3])
+def test_append_index_keys(es):
+    """Keys into the ragged array of the indexer, whole entries only."""
+    hist, new = [50, 3, 1000], [9, 30, 64]
+    bt = janus.Batch(hist, new, entry_shift=es)
+    x, xd = _inputs(103, 1, 128, "bf16", 8)
+    y = rotate(xd, positions(hist, new), _freq(64)[0], 0, "half")[0][:, 0]
+    keys = torch.full((bt.total_ctx, 128), 9, dtype=torch.uint8, device="cuda")
+    scale = torch.full((bt.total_ctx,), -1.0, device="cuda")
+    janus.kv_append(bt, x[:, 0], keys, janus.Rotary(64), out_scale=scale)
+    at, tokens = [], []
+    for b, (M, N) in enumerate(zip(hist, new)):
+        for i in range(N):
+            if (M + i + 1) % (1 << es) == 0:
+                at.append(int(bt.ctx_start_host[b]) + ((M + i + 1) >> es) - 1)
+                tokens.append(int(bt.q_start_host[b]) + i)
+    _close_fp8(_fp8(keys)[at], scale[at], y[tokens])
+    left = np.setdiff1d(np.arange(bt.total_ctx), at)
+    assert (keys[left] == 9).all() and (scale[left] == -1).all()
+
+
+def test_far_rows():
+    """Rows beyond 2^31 bytes of the pool."""
+    T = 5
+    x, xd = _inputs(T, 1, 576, "bf16", 8)
+    pool = torch.empty((4_000_000, 592), dtype=torch.uint8, device="cuda")
+    rows = np.array([3_999_999, 0, 3_700_001, 3_627_505, 12], np.int64)
+    janus.kv_append(janus.Batch([9], [T]), x[:, 0], pool, janus.Rotary(64, 512), rows=torch.from_numpy(rows).cuda())
+    got = pool[torch.from_numpy(rows).cuda()]
+    want = rotate(xd, positions([9], [T]), _freq(64)[0], 512, "half")[0][:, 0]
+    _close_fp8(_fp8(got[:, :576].contiguous()), got[:, 576:580].contiguous().view(torch.float32)[:, 0], want)
+
+
+def test_another_stream_and_replays():
+    x, xd = _inputs(33, 8, 128, "bf16", 3)
+    want, mass = rotate(xd, positions([500], [33]), _freq(128)[0], 0, "half")
+    bt, rot, out = janus.Batch([500], [33]), janus.Rotary(128), torch.zeros_like(x)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    janus.rope(bt, rot, x, out=out, stream=side)
+    side.synchronize()
+    _close(out, want, mass, "bf16")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        janus.rope(bt, rot, x, out=out)
+    for k in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        _close(out, want, mass, "bf16")
