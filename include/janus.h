@@ -517,15 +517,16 @@ int janus_kv_append(const janus_batch *b, const janus_rotary *r, const void *x, 
  * ceil(prefix_len / page_size) entries of each session that reads them give
  * pages with the same contents there (usually the same pages; the page the
  * prefix ends in may be a copy).  Where that pays, rows of different
- * sessions meet the prefix's keys together, through table row 0, and their own ids apart,
- * joined by their maxima and sums.  prefix_len = 0 is any ragged batch.
+ * sessions meet the prefix's keys together, through table row 0 (which has all
+ * of those entries, however short session 0 is), and their own ids apart, joined
+ * by their maxima and sums.  prefix_len = 0 is any ragged batch.
  *   prefix_len      0 .. max_ctx, in ids
  *   q, pools, strides, page_table, softmax_scale, out, lse: as janus_sparse_attn
  *   workspace, workspace_bytes: as janus_sparse_attn_split
  * Shapes: MLA (dqk = 576, dv = 512, v_pool == k_pool, equal strides) and MQA
  * (dqk = dv = 128), each with 1 <= Hq <= 128, q and pools 16-byte aligned and
- * row strides in multiples of 8, total_q * Hq < 2^31; else JANUS_ERR_UNSUPPORTED.  A
- * workspace that is used must be 16-byte aligned, and out 4-byte aligned (else
+ * row strides in multiples of 8 up to 2^24, total_q * Hq < 2^31; else
+ * JANUS_ERR_UNSUPPORTED.  A workspace that is used must be 16-byte aligned, and out 4-byte aligned (else
  * JANUS_ERR_UNSUPPORTED).  A token with no candidate gets out = 0 and lse = -inf.  Rows from
  * q_start[B] on are left as they are.  Ids that a token does not attend to
  * do not touch its result, whatever their rows hold.

@@ -45,66 +45,93 @@ struct PrefixArgs {
     PrefixPlan plan;
 };
 
-// Exchange of a row's 16-byte chunks: chunk c of row r lies at c ^ swz(r).
-// Eight rows of four neighbouring chunks (a transposing read) and sixteen rows
-// of one (a K read) then spread over the banks evenly.  Rows of 256 bytes begin in
-// the same bank; MLA rows (4.5 x 256) alternate between two halves.
-template <int RB>
-JANUS_DEV int swz(int r)
+// The block's rows, keys and table.
+struct PrefixRange {
+    int row0, row1, kbeg, kend, sess, slot;
+    bool shared;
+};
+JANUS_DEV PrefixRange prefix_range(const PrefixArgs &g, int64_t blk)
 {
-    if constexpr (RB % 256 == 0)
-        return ((r & 1) << 3) | ((r & 2) << 1) | ((r & 4) >> 1) | ((r & 8) >> 3);
-    else
-        return ((r & 2) << 1) | ((r & 4) >> 1) | ((r & 8) >> 3);
+    const PrefixBlock bk = prefix_block(g.plan, blk);
+    PrefixRange r;
+    r.shared = bk.shared;
+    r.slot = bk.slot;
+    r.sess = 0;
+    if (bk.shared) {
+        r.row0 = bk.tile * PA_ROWS;
+        r.row1 = min(r.row0 + PA_ROWS, g.q_start[g.num_seqs] * g.heads);
+        r.kbeg = bk.chunk * g.plan.chunk;
+        r.kend = min(r.kbeg + g.plan.chunk, g.plan.prefix);
+        return r;
+    }
+    int lo = 0, hi = g.num_seqs - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (prefix_tile_first(g.q_start[mid], g.heads, mid) <= bk.tile)
+            lo = mid;
+        else
+            hi = mid - 1;
+    }
+    const int q0 = g.q_start[lo], q1 = g.q_start[lo + 1];
+    r.sess = lo;
+    r.row0 = q0 * g.heads + (bk.tile - prefix_tile_first(q0, g.heads, lo)) * PA_ROWS;
+    r.row1 = min(r.row0 + PA_ROWS, q1 * g.heads);
+    r.kbeg = g.plan.prefix + bk.chunk * g.plan.chunk;
+    r.kend = r.row0 < r.row1
+                 ? min(r.kbeg + g.plan.chunk, last_cand(g.hist_len[lo], (r.row1 - 1) / g.heads - q0, g.es) + 1)
+                 : r.kbeg;
+    return r;
+}
+// First key that the row's token does not attend to.
+JANUS_DEV int row_limit(const PrefixArgs &g, const PrefixRange &r, int row)
+{
+    const int token = row / g.heads;
+    const int s = r.shared ? session_of_row(g.q_start, g.num_seqs, token) : r.sess;
+    return min(r.kend, last_cand(g.hist_len[s], token - g.q_start[s], g.es) + 1);
 }
 
-template <int DQK, int DV, bool ONE, int KT, int NBUF>
-__global__ __launch_bounds__(PA_THREADS, 1) void prefix_attn(PrefixArgs g)
+// Parts of a bf16 pair word of V that are not finite: what is left, and the
+// largest finite value in the place of +inf or NaN (up), of -inf or NaN (down).
+JANUS_DEV void split_odd(int x, int &fin, int &up, int &down)
 {
-    constexpr int KRB = DQK * 2, VRB = ONE ? KRB : DV * 2;  // bytes of a row in LDS
-    constexpr int KBUF = KT * KRB, BUF = KBUF + (ONE ? 0 : KT * VRB);
-    constexpr int KI = KBUF / (1024 * PA_WAVES), VI = ONE ? 0 : KT * VRB / (1024 * PA_WAVES);
-    constexpr int STEPS = DQK / 16, NB = DV / 32, NK = KT / 32;
-    static_assert(KI * 1024 * PA_WAVES == KBUF, "whole gathers");
-    __shared__ __attribute__((aligned(16))) uint8_t ring[NBUF * BUF];
+    fin = up = down = 0;
+#pragma unroll
+    for (int z = 0; z < 32; z += 16) {
+        const int v = x >> z & 0xffff;
+        const bool bad = (v & 0x7f80) == 0x7f80;
+        fin |= bad ? 0 : v << z;
+        up |= bad && v != 0xff80 ? 0x7f7f << z : 0;
+        down |= bad && v != 0x7f80 ? 0xff7f << z : 0;
+    }
+}
+
+// Within a row in LDS, chunk c (16 bytes) of row r lies at c ^ swz16(r), in rows of 16
+// chunks and more, and at c ^ swz8(r) in rows of eight.  Sixteen rows of one chunk (a K
+// read), and four rows of four neighbouring ones (a transposing read), then lie in
+// banks of their own.
+JANUS_DEV int swz16(int r) { return ((r & 1) << 3) | ((r & 2) << 1) | ((r & 4) >> 1) | ((r & 8) >> 3); }
+JANUS_DEV int swz8(int r) { return ((r & 2) << 1) | ((r & 4) >> 1) | ((r & 8) >> 3); }
+
+constexpr int PQ_KT = 64;  // keys of a tile
+
+__global__ __launch_bounds__(PA_THREADS, 1) void prefix_mqa(PrefixArgs g)
+{
+    constexpr int RB = 256, CH = 16;                     // bytes and chunks of a row
+    constexpr int KBUF = PQ_KT * RB, BUF = 2 * KBUF;     // K rows, then V rows
+    constexpr int STEPS = 8, NB = 4, NK = PQ_KT / 32;    // K-steps, blocks of 32 dims and of 32 keys
+    constexpr int GATHERS = KBUF / (1024 * PA_WAVES);    // a wave's, of each pool
+    __shared__ __attribute__((aligned(16))) uint8_t ring[2 * BUF];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c32 = lane & 31, hf = lane >> 5;
-    const PrefixBlock bk = prefix_block(g.plan, blockIdx.x);
-    // the block's rows, keys [kbeg, kend) and table
-    int row0, row1, kbeg, kend, sess = 0;
-    if (bk.shared) {
-        row0 = bk.tile * PA_ROWS;
-        row1 = min(row0 + PA_ROWS, g.q_start[g.num_seqs] * g.heads);
-        kbeg = bk.chunk * g.plan.chunk;
-        kend = min(kbeg + g.plan.chunk, g.plan.prefix);
-    } else {
-        int lo = 0, hi = g.num_seqs - 1;
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (prefix_tile_first(g.q_start[mid], g.heads, mid) <= bk.tile)
-                lo = mid;
-            else
-                hi = mid - 1;
-        }
-        sess = lo;
-        const int q0 = g.q_start[sess], q1 = g.q_start[sess + 1];
-        row0 = q0 * g.heads + (bk.tile - prefix_tile_first(q0, g.heads, sess)) * PA_ROWS;
-        row1 = min(row0 + PA_ROWS, q1 * g.heads);
-        if (row0 >= row1)
-            return;
-        kbeg = g.plan.prefix + bk.chunk * g.plan.chunk;
-        kend = min(kbeg + g.plan.chunk, last_cand(g.hist_len[sess], (row1 - 1) / g.heads - q0, g.es) + 1);
-    }
-    if (row0 >= row1)
+    const PrefixRange r = prefix_range(g, blockIdx.x);
+    if (r.row0 >= r.row1)
         return;
-    const int32_t *pt = g.table + (int64_t)sess * g.pt_ld;
-    // this lane's row and the end of its keys
-    const int row = row0 + 32 * wave + c32;
-    const bool live = row < row1;
-    const int token = (live ? row : row1 - 1) / g.heads;
-    const int mine = bk.shared ? session_of_row(g.q_start, g.num_seqs, token) : sess;
-    const int lim = min(kend, last_cand(g.hist_len[mine], token - g.q_start[mine], g.es) + 1);
+    const int32_t *pt = g.table + (int64_t)r.sess * g.pt_ld;
+    const int kbeg = r.kbeg, kend = r.kend;
+    const int row = r.row0 + 32 * wave + c32;
+    const bool live = row < r.row1;
+    const int lim = row_limit(g, r, live ? row : r.row1 - 1);
     int wmin = live ? lim : 0x7fffffff;  // keys before it are every row's of the wave
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1)
@@ -113,7 +140,7 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_attn(PrefixArgs g)
 
     v8bf qf[STEPS];
     {
-        const uint16_t *qr = g.q + (int64_t)(live ? row : row1 - 1) * DQK + 8 * hf;
+        const uint16_t *qr = g.q + (int64_t)(live ? row : r.row1 - 1) * 128 + 8 * hf;
 #pragma unroll
         for (int st = 0; st < STEPS; ++st)
             qf[st] = as_v8bf(*(const v4i *)(qr + 16 * st));
@@ -126,52 +153,44 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_attn(PrefixArgs g)
             o[d][i] = 0.f;
     float m = M_INIT, lsum = 0.f;
 
-    // Tiles begin at multiples of KT: a tile of a page of at least KT ids lies
-    // in one page.  Keys outside [kbeg, kend) load the nearest one inside.
-    const int base0 = kbeg & ~(KT - 1);
-    const int nt = kend > kbeg ? (kend - base0 + KT - 1) / KT : 0;
-    const bool one_page = (1 << g.page_shift) >= KT;
+    // Tiles begin at multiples of their length: a tile of longer pages lies in one.
+    // Keys outside [kbeg, kend) load the nearest one inside.
+    const int base0 = kbeg & ~(PQ_KT - 1);
+    const int nt = kend > kbeg ? (kend - base0 + PQ_KT - 1) / PQ_KT : 0;
+    const bool one_page = (1 << g.page_shift) >= PQ_KT;
     auto slot_of = [&](int key) {
         return ((int64_t)pt[key >> g.page_shift] << g.page_shift) + (key & ((1 << g.page_shift) - 1));
     };
     auto issue = [&](int t) {
-        uint8_t *dst = ring + (t % NBUF) * BUF;
-        const int base = base0 + t * KT;
-        const int first = max(kbeg - base, 0), last = min(kend - base, KT) - 1;
+        uint8_t *dst = ring + (t & 1) * BUF;
+        const int base = base0 + t * PQ_KT;
+        const int first = max(kbeg - base, 0), last = min(kend - base, PQ_KT) - 1;
         const int64_t slot0 = one_page ? slot_of(base) : 0;
 #pragma unroll
-        for (int j = 0; j < KI + VI; ++j) {
-            const bool isv = j >= KI;
-            const int rb16 = (isv ? VRB : KRB) / 16;
-            const int at = 64 * (wave + PA_WAVES * (isv ? j - KI : j));
-            const int p = at + lane, r = p / rb16, c = p - r * rb16;
-            const int rr = min(max(r, first), last);
-            const int64_t slot = one_page ? slot0 + rr : slot_of(base + rr);
-            const uint8_t *src = (isv ? g.v : g.k) + slot * (isv ? g.v_rb : g.k_rb) +
-                                 16 * (isv ? c ^ swz<VRB>(r) : c ^ swz<KRB>(r));
+        for (int j = 0; j < 2 * GATHERS; ++j) {
+            const bool isv = j >= GATHERS;
+            const int at = 64 * (wave + PA_WAVES * (isv ? j - GATHERS : j));
+            const int k = (at + lane) / CH, c = (at + lane) % CH;
+            const int kk = min(max(k, first), last);
+            const int64_t slot = one_page ? slot0 + kk : slot_of(base + kk);
+            const uint8_t *src = (isv ? g.v : g.k) + slot * (isv ? g.v_rb : g.k_rb) + 16 * (c ^ swz16(k));
             gather16(src, dst + (isv ? KBUF : 0) + 16 * at);
         }
     };
-#pragma unroll
-    for (int t = 0; t < NBUF - 1; ++t)
-        if (t < nt)
-            issue(t);
+    if (nt > 0)
+        issue(0);
 
-    const int kcol = (hf ^ swz<KRB>(c32)) * 16;  // K: chunk 2 st + hf of key c32
+    const int kcol = (hf ^ swz16(c32)) * 16;  // K: chunk 2 st + hf of key c32
     // V: this lane addresses key 16 s + 8 u + 4 hf + (lane / 4) % 4 and dims 32 d + 16 (lane / 16 % 2) + 4 (lane % 4)
     const int vkey = 4 * hf + ((lane >> 2) & 3);
     const int vch = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
     for (int t = 0; t < nt; ++t) {
-        if (NBUF > 2 && t + 1 < nt)
-            __builtin_amdgcn_s_waitcnt(vmcnt_only(KI + VI));
-        else
-            __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
+        __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
         lds_barrier();
-        if (t + NBUF - 1 < nt)
-            issue(t + NBUF - 1);
-        const uint8_t *tile = ring + (t % NBUF) * BUF;
-        const uint8_t *vt = ONE ? tile : tile + KBUF;
-        const int base = base0 + t * KT;
+        if (t + 1 < nt)
+            issue(t + 1);
+        const uint8_t *tile = ring + (t & 1) * BUF, *vt = tile + KBUF;
+        const int base = base0 + t * PQ_KT;
 
         // K operands are read AHEAD steps before their MFMA, with a scheduling
         // fence a step: the compiler alone hoists as many reads as it finds, and spills.
@@ -179,12 +198,8 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_attn(PrefixArgs g)
         {
             constexpr int AHEAD = 4, ALL = NK * STEPS;
             auto kop = [&](int x) {
-                // step x / NK of keys 32 (x % NK) + c32; chunk 2 st + hf, exchanged: the low bits
-                // by xor, the others as they are
-                constexpr int LOW = KRB % 256 == 0 ? 8 : 4;  // steps whose chunks the exchange mixes
-                const int st = x / NK;
-                return *(const v4i *)(tile + (32 * (x % NK) + c32) * KRB + (kcol ^ (32 * (st % LOW))) +
-                                      32 * (st - st % LOW));
+                // step x / NK of keys 32 (x % NK) + c32
+                return *(const v4i *)(tile + (32 * (x % NK) + c32) * RB + (kcol ^ (32 * (x / NK))));
             };
             v4i ahead[AHEAD];
 #pragma unroll
@@ -205,7 +220,7 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_attn(PrefixArgs g)
             }
         }
         // keys 32 kb + 8 (i / 4) + 4 hf + i % 4 of this lane's row
-        const bool whole = base >= kbeg && base + KT <= wmin && g.scale_log2 > 0.f;
+        const bool whole = base >= kbeg && base + PQ_KT <= wmin && g.scale_log2 > 0.f;
         float mx = -INFINITY, mult = g.scale_log2;
         if (whole) {
 #pragma unroll
@@ -255,8 +270,8 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_attn(PrefixArgs g)
             v4s16 part[2];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const int r = 16 * h + 8 * u + vkey;
-                part[u] = lds_read_tr16(vt, r * VRB + 16 * ((4 * d + vch) ^ swz<VRB>(8 * u + vkey)) + 8 * (lane & 1));
+                const int k = 16 * h + 8 * u + vkey;
+                part[u] = lds_read_tr16(vt, k * RB + 16 * ((4 * d + vch) ^ swz16(8 * u + vkey)) + 8 * (lane & 1));
             }
             __builtin_memcpy(&a, part, 16);
             return a;
@@ -271,7 +286,7 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_attn(PrefixArgs g)
         if (!whole) {
             int bad = 0;
 #pragma unroll 4
-            for (int w = 0; w < KT * VRB / 1024; ++w) {
+            for (int w = 0; w < KBUF / 1024; ++w) {
                 const v4i x = *(const v4i *)(vt + 1024 * w + 16 * lane);
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
@@ -304,18 +319,14 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_attn(PrefixArgs g)
 #pragma unroll
                 for (int d = 0; d < NB; ++d) {
                     const v4i a = __builtin_bit_cast(v4i, vop(h, d));
-                    v4i fin, up, down;  // finite values; +inf or NaN; -inf or NaN
+                    v4i fin, up, down;
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {
-                        fin[w] = up[w] = down[w] = 0;
-#pragma unroll
-                        for (int z = 0; z < 32; z += 16) {
-                            const int x = a[w] >> z & 0xffff;
-                            const bool bad = (x & 0x7f80) == 0x7f80;
-                            fin[w] |= bad ? 0 : x << z;
-                            up[w] |= bad && x != 0xff80 ? 0x7f7f << z : 0;
-                            down[w] |= bad && x != 0x7f80 ? 0xff7f << z : 0;
-                        }
+                        int x, y, z;
+                        split_odd(a[w], x, y, z);
+                        fin[w] = x;
+                        up[w] = y;
+                        down[w] = z;
                     }
                     o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_v8bf(fin), pb[h], o[d], 0, 0, 0);
                     o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_v8bf(up), as_v8bf(has), o[d], 0, 0, 0);
@@ -330,15 +341,15 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_attn(PrefixArgs g)
     if (!live)
         return;
     if (g.part) {
-        const int64_t at = (int64_t)bk.slot * g.plan.rows + row;
+        const int64_t at = (int64_t)r.slot * g.plan.rows + row;
         if (hf == 0)
-            *(float2 *)(g.part + (int64_t)g.plan.slots * g.plan.rows * DV + 2 * at) = float2{m, l};
+            *(float2 *)(g.part + (int64_t)g.plan.slots * g.plan.rows * 128 + 2 * at) = float2{m, l};
         if (nt > 0) {
 #pragma unroll
             for (int d = 0; d < NB; ++d)
 #pragma unroll
                 for (int i = 0; i < 16; i += 4)
-                    *(v4f *)(g.part + at * DV + 32 * d + 2 * i + 4 * hf) =
+                    *(v4f *)(g.part + at * 128 + 32 * d + 2 * i + 4 * hf) =
                         v4f{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
         }
         return;
@@ -348,10 +359,386 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_attn(PrefixArgs g)
     for (int d = 0; d < NB; ++d)
 #pragma unroll
         for (int i = 0; i < 16; i += 4)
-            store_out4(g.out, g.out_f32, (int64_t)row * DV + 32 * d + 2 * i + 4 * hf,
+            store_out4(g.out, g.out_f32, (int64_t)row * 128 + 32 * d + 2 * i + 4 * hf,
                        v4f{o[d][i] * inv, o[d][i + 1] * inv, o[d][i + 2] * inv, o[d][i + 3] * inv});
     if (g.lse && hf == 0)
         g.lse[row] = l != 0.f ? (m + log2f(l)) * LN2 : -INFINITY;
+}
+
+// The block's rows without matrix instructions, a wave a row and a lane a key, then eight dims.
+JANUS_DEV void plain_rows(const PrefixArgs &g, const PrefixRange &r, const int *lim)
+{
+    const int lane = threadIdx.x & 63;
+    const int32_t *pt = g.table + (int64_t)r.sess * g.pt_ld;
+    auto key_row = [&](int key) {
+        return (const uint16_t *)(g.k + (((int64_t)pt[key >> g.page_shift] << g.page_shift) +
+                                         (key & ((1 << g.page_shift) - 1))) * g.k_rb);
+    };
+    for (int row = r.row0 + (threadIdx.x >> 6); row < r.row1; row += PA_WAVES) {
+        const uint16_t *q = g.q + (int64_t)row * 576;
+        const int end = lim[row - r.row0];
+        float m = M_INIT, l = 0.f, acc[8] = {};
+        for (int k0 = r.kbeg; k0 < end; k0 += 64) {
+            float x = -INFINITY;
+            if (k0 + lane < end) {
+                const uint16_t *k = key_row(k0 + lane);
+                x = 0.f;
+                for (int e = 0; e < 576; ++e)
+                    x = fmaf(bf16_to_f32(q[e]), bf16_to_f32(k[e]), x);
+                x *= g.scale_log2;
+            }
+            float top = x;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1)
+                top = fmaxf(top, __shfl_xor(top, o));
+            const float mnew = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f(m - mnew);
+            m = mnew;
+            const float p = k0 + lane < end ? __builtin_amdgcn_exp2f(x - m) : 0.f;
+            l *= alpha;
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                acc[e] *= alpha;
+            for (int j = 0; j < min(64, end - k0); ++j) {
+                const float pj = __shfl(p, j);
+                const uint16_t *v = key_row(k0 + j) + 8 * lane;
+                l += pj;
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    acc[e] = fmaf(pj, bf16_to_f32(v[e]), acc[e]);
+            }
+        }
+        const v4f a = {acc[0], acc[1], acc[2], acc[3]}, b = {acc[4], acc[5], acc[6], acc[7]};
+        if (g.part) {
+            const int64_t at = (int64_t)r.slot * g.plan.rows + row;
+            *(v4f *)(g.part + at * 512 + 8 * lane) = a;
+            *(v4f *)(g.part + at * 512 + 8 * lane + 4) = b;
+            if (lane == 0)
+                *(float2 *)(g.part + (int64_t)g.plan.slots * g.plan.rows * 512 + 2 * at) = float2{m, l};
+        } else {
+            const float inv = l != 0.f ? 1.f / l : 0.f;
+            store_out4(g.out, g.out_f32, (int64_t)row * 512 + 8 * lane, a * inv);
+            store_out4(g.out, g.out_f32, (int64_t)row * 512 + 8 * lane + 4, b * inv);
+            if (g.lse && lane == 0)
+                g.lse[row] = l != 0.f ? (m + log2f(l)) * LN2 : -INFINITY;
+        }
+    }
+}
+
+constexpr int PM_KT = 32, PM_STEPS = 576 / 16;
+constexpr int PM_MAIN = PM_KT * 1024, PM_BUF = PM_MAIN + PM_KT * 128;  // dims 0..511, then 512..575
+// A row's maximum is that of its first tile, and probabilities may exceed 1 by this
+// much (log2): nothing is lost, their exponents have room.  Rows that outgrow it
+// are done again from their maxima, so that O is never rescaled.
+constexpr float PM_HEADROOM = 32.f;
+
+// S^T on registers that are not accumulators: O fills all 256 of those, and the
+// compiler would put S among them.  It inserts no wait states for assembly: two
+// before an MFMA whose sources the VALU may have written, and what reads S
+// waits by itself (settled).
+JANUS_DEV void mfma_first(v16f &s, v4i a, v8bf b)
+{
+    asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(s) : "v"(a), "v"(b));
+}
+JANUS_DEV void mfma_next(v16f &s, v4i a, v8bf b)
+{
+    asm("s_nop 1\n\tv_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+v"(s) : "v"(a), "v"(b));
+}
+JANUS_DEV void settled(v16f &s) { asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s)); }
+
+__global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
+{
+    __shared__ __attribute__((aligned(16))) uint8_t ring[3 * PM_BUF];
+    __shared__ v4i sP[2][PA_WAVES][2][64];       // probabilities of the waves' rows, as operands
+    __shared__ v4i sOver;                        // a wave's rows outgrew their maxima
+    __shared__ int sLim[PA_ROWS];
+    __shared__ float sM[PA_ROWS], sL[PA_ROWS];
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int c32 = lane & 31, hf = lane >> 5;
+    const PrefixRange r = prefix_range(g, blockIdx.x);
+    if (r.row0 >= r.row1)
+        return;
+    typedef const __attribute__((address_space(4))) int32_t *scalar_i32;  // read through the scalar cache
+    const scalar_i32 pt = (scalar_i32)(g.table + (int64_t)r.sess * g.pt_ld);
+    const int kbeg = r.kbeg, kend = r.kend;
+    const int row = r.row0 + 32 * wave + c32;
+    const bool live = row < r.row1;
+    const int lim = row_limit(g, r, live ? row : r.row1 - 1);
+    if (hf == 0)
+        sLim[32 * wave + c32] = lim;
+
+    v8bf qf[PM_STEPS];
+    {
+        const uint16_t *qr = g.q + (int64_t)(live ? row : r.row1 - 1) * 576 + 8 * hf;
+#pragma unroll
+        for (int st = 0; st < PM_STEPS; ++st)
+            qf[st] = as_v8bf(*(const v4i *)(qr + 16 * st));
+    }
+    // O^T of dims 128 wave + 32 d .. and rows 32 rb ..
+    v16f o[4][PA_WAVES];
+    float m = M_INIT, lsum = 0.f;
+
+    const int base0 = kbeg & ~(PM_KT - 1);
+    const int nt = kend > kbeg ? (kend - base0 + PM_KT - 1) / PM_KT : 0;
+    const int ps = (1 << g.page_shift) - 1;
+    const uint32_t rb32 = (uint32_t)g.k_rb;
+    auto key_row = [&](int key) {  // (uniform)
+        return g.k + (((int64_t)pt[key >> g.page_shift] << g.page_shift) + (key & ps)) * (int64_t)rb32;
+    };
+    // Wave w gathers rows 8 w .. 8 w + 7: dims 0..511 a row at a time (64 lanes of 16
+    // bytes), the last 64 dims of the eight together.
+    const int tr = lane >> 3;
+    auto issue = [&](int t) {
+        uint8_t *dst = ring + (t % 3) * PM_BUF;
+        const int key0 = base0 + t * PM_KT + 8 * wave;
+        if (g.page_shift >= 3 && key0 >= kbeg && key0 + 8 <= kend) {
+            const uint8_t *src = key_row(key0);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                gather16(src + i * (int64_t)rb32, 16u * (lane ^ swz16(8 * (wave & 1) + i)), dst + 1024 * (8 * wave + i));
+            gather16(src, tr * rb32 + 1024u + 16u * ((lane & 7) ^ swz8(8 * (wave & 1) + tr)),
+                     dst + PM_MAIN + 1024 * wave);
+        } else {
+            // keys outside [kbeg, kend) load the nearest one inside
+            const uint8_t *mine = g.k;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint8_t *src = key_row(min(max(key0 + i, kbeg), kend - 1));
+                gather16(src, 16u * (lane ^ swz16(8 * (wave & 1) + i)), dst + 1024 * (8 * wave + i));
+                mine = tr == i ? src : mine;
+            }
+            gather16(mine + 1024 + 16 * ((lane & 7) ^ swz8(8 * (wave & 1) + tr)), dst + PM_MAIN + 1024 * wave);
+        }
+    };
+    if (nt > 0)
+        issue(0);
+
+    const int kcol = (hf ^ swz16(c32)) * 16, tcol = (hf ^ swz8(c32)) * 16;
+    const int vkey = 4 * hf + ((lane >> 2) & 3);
+    const int vch = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+    v16f s;
+    v8bf pb[2];
+    __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
+    lds_barrier();
+    int bmin;  // keys before it are every row's of the block
+    {
+        const int a = r.row0 + lane < r.row1 ? sLim[lane] : 0x7fffffff;
+        const int b = r.row0 + 64 + lane < r.row1 ? sLim[64 + lane] : 0x7fffffff;
+        bmin = min(a, b);
+#pragma unroll
+        for (int x = 1; x < 64; x <<= 1)
+            bmin = min(bmin, __shfl_xor(bmin, x));
+        bmin = __builtin_amdgcn_readfirstlane(bmin);
+    }
+    int bad = 0;  // a tile where rows end holds values of V that are not finite
+
+    // S^T of tile t; K operands are read AHEAD steps before their MFMA
+    auto logits = [&](int t) {
+        const uint8_t *tile = ring + (t % 3) * PM_BUF;
+        constexpr int AHEAD = 4;
+        auto kop = [&](int st) {
+            return st < 32 ? *(const v4i *)(tile + c32 * 1024 + (kcol ^ (32 * (st & 7))) + 256 * (st >> 3))
+                           : *(const v4i *)(tile + PM_MAIN + c32 * 128 + (tcol ^ (32 * (st & 3))));
+        };
+        v4i ahead[AHEAD];
+#pragma unroll
+        for (int x = 0; x < AHEAD; ++x)
+            ahead[x] = kop(x);
+#pragma unroll
+        for (int st = 0; st < PM_STEPS; ++st) {
+            if (st == 0)
+                mfma_first(s, ahead[0], qf[0]);
+            else
+                mfma_next(s, ahead[st % AHEAD], qf[st]);
+            if (st + AHEAD < PM_STEPS)
+                ahead[st % AHEAD] = kop(st + AHEAD);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // The logits of tile t scaled, those of keys that a row does not have -inf;
+    // returns the factor that is left to apply.
+    auto mask = [&](int t) {
+        settled(s);
+        const int base = base0 + t * PM_KT;
+        const bool inside = base >= kbeg && base + PM_KT <= bmin;
+        if (inside && g.scale_log2 > 0.f)
+            return g.scale_log2;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int key = base + 8 * (i / 4) + 4 * hf + i % 4;
+            s[i] = key >= kbeg && key < lim ? s[i] * g.scale_log2 : -INFINITY;
+        }
+        if (!inside) {
+            const uint8_t *tile = ring + (t % 3) * PM_BUF;
+#pragma unroll 2
+            for (int w = 0; w < 8; ++w) {
+                const v4i x = *(const v4i *)(tile + 1024 * (4 * w + (lane >> 4)) + 256 * wave + 16 * (lane & 15));
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    bad |= (x[e] & 0x7f80) == 0x7f80 || (x[e] & 0x7f800000) == 0x7f800000;
+            }
+        }
+        return 1.f;
+    };
+    // Probabilities of s * mult (mult > 0), relative to the maximum of the first
+    // tile that has keys of the row.
+    bool over = false;
+    auto probabilities = [&](float mult) {
+        float mx = s[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i)
+            mx = fmaxf(mx, s[i]);
+        mx *= mult;
+        if (__ballot(mx > m + PM_HEADROOM) != 0) {
+            mx = fmaxf(mx, __shfl_xor(mx, 32));
+            over |= m != M_INIT && mx > m + PM_HEADROOM;
+            m = m == M_INIT ? fmaxf(mx, M_INIT) : m;
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            v8f p;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                p[e] = __builtin_amdgcn_exp2f(s[8 * h + e] * mult - m);
+                lsum += p[e];
+            }
+            pb[h] = __builtin_convertvector(p, v8bf);
+        }
+    };
+    auto give = [&](int t) {
+        sP[t & 1][wave][0][lane] = __builtin_bit_cast(v4i, pb[0]);
+        sP[t & 1][wave][1][lane] = __builtin_bit_cast(v4i, pb[1]);
+        __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
+        lds_barrier();
+    };
+    // O += P V of tile t, this wave's dims
+    auto product = [&](int t) {
+        const uint8_t *vt = ring + (t % 3) * PM_BUF + 256 * wave;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            v8bf p[PA_WAVES];
+#pragma unroll
+            for (int rb = 0; rb < PA_WAVES; ++rb)
+                p[rb] = as_v8bf(sP[t & 1][rb][h][lane]);
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                // keys 16 h + .., dims 128 wave + 32 d + ..
+                v4s16 part[2];
+                v8bf a;
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const int k = 16 * h + 8 * u + vkey;
+                    part[u] = lds_read_tr16(vt, k * 1024 + 16 * ((4 * d + vch) ^ swz16(8 * u + vkey)) + 8 * (lane & 1));
+                }
+                __builtin_memcpy(&a, part, 16);
+#pragma unroll
+                for (int rb = 0; rb < PA_WAVES; ++rb)
+                    o[d][rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, p[rb], o[d][rb], 0, 0, 0);
+            }
+        }
+    };
+    if (nt > 0) {
+        // The second time round, the rows' maxima over all their keys are known.
+#pragma unroll 1
+        for (int round = 0; round < 2; ++round) {
+#pragma unroll
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int rb = 0; rb < PA_WAVES; ++rb)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        o[d][rb][i] = 0.f;
+            lsum = 0.f;
+            if (nt > 1)
+                issue(1);
+            logits(0);
+            probabilities(mask(0));
+            give(0);
+#pragma unroll 1
+            for (int t = 1; t < nt; ++t) {
+                if (t + 1 < nt)
+                    issue(t + 1);
+                logits(t);
+                probabilities(mask(t));
+                product(t - 1);
+                give(t);
+            }
+            product(nt - 1);
+            if (lane == 0)
+                ((int *)&sOver)[wave] = 0;
+            if (__ballot(over) != 0 && lane == 0)
+                ((int *)&sOver)[wave] = 1;
+            lds_barrier();
+            const v4i any = sOver;
+            if (round || !__builtin_amdgcn_readfirstlane(any[0] | any[1] | any[2] | any[3]))
+                break;
+            over = false;
+            issue(0);
+            __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
+            lds_barrier();
+#pragma unroll 1
+            for (int t = 0; t < nt; ++t) {
+                if (t + 1 < nt)
+                    issue(t + 1);
+                logits(t);
+                const float mult = mask(t);
+                float mx = s[0];
+#pragma unroll
+                for (int i = 1; i < 16; ++i)
+                    mx = fmaxf(mx, s[i]);
+                m = fmaxf(m, mx * mult);
+                __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
+                lds_barrier();
+            }
+            m = fmaxf(m, __shfl_xor(m, 32));
+            issue(0);
+            __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
+            lds_barrier();
+        }
+    }
+
+    // Rows that end in a tile whose V holds an infinity or NaN: a probability of 0
+    // does not undo it.  The block is done again, a row and a key at a time.
+    if (__syncthreads_or(bad)) {
+        plain_rows(g, r, sLim);
+        return;
+    }
+    const float l = lsum + __shfl_xor(lsum, 32);
+    if (hf == 0) {
+        sM[32 * wave + c32] = m;
+        sL[32 * wave + c32] = l;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int rb = 0; rb < PA_WAVES; ++rb) {
+        const int at = 32 * rb + c32, to = r.row0 + at;
+        if (to >= r.row1)
+            continue;
+        const float mm = sM[at], ll = sL[at];
+        if (g.part) {
+            const int64_t slot = (int64_t)r.slot * g.plan.rows + to;
+            if (hf == 0 && wave == 0)
+                *(float2 *)(g.part + (int64_t)g.plan.slots * g.plan.rows * 512 + 2 * slot) = float2{mm, ll};
+            if (nt > 0) {
+#pragma unroll
+                for (int d = 0; d < 4; ++d)
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4)
+                        *(v4f *)(g.part + slot * 512 + 128 * wave + 32 * d + 2 * i + 4 * hf) =
+                            v4f{o[d][rb][i], o[d][rb][i + 1], o[d][rb][i + 2], o[d][rb][i + 3]};
+            }
+            continue;
+        }
+        const float inv = ll != 0.f ? 1.f / ll : 0.f;
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                store_out4(g.out, g.out_f32, (int64_t)to * 512 + 128 * wave + 32 * d + 2 * i + 4 * hf,
+                           v4f{o[d][rb][i] * inv, o[d][rb][i + 1] * inv, o[d][rb][i + 2] * inv, o[d][rb][i + 3] * inv});
+        if (g.lse && hf == 0 && wave == 0)
+            g.lse[to] = ll != 0.f ? (mm + log2f(ll)) * LN2 : -INFINITY;
+    }
 }
 
 // Joins the ranges of a row: with maxima m_s and sums l_s, M = max m_s and w_s =
@@ -410,7 +797,7 @@ extern "C" int janus_prefix_attn(const janus_batch *bt, const void *q, int Hq, i
     const bool mla = dqk == 576 && dv == 512 && v_pool == k_pool && k_row_stride == v_row_stride;
     const bool mqa = dqk == 128 && dv == 128;
     if ((out_dt != JANUS_BF16 && out_dt != JANUS_F32) || (!mla && !mqa) || Hq > 128 || k_row_stride % 8 != 0 ||
-        v_row_stride % 8 != 0 || k_row_stride > (1 << 30) || v_row_stride > (1 << 30) || !at(q, 16) ||
+        v_row_stride % 8 != 0 || k_row_stride > (1 << 24) || v_row_stride > (1 << 24) || !at(q, 16) ||
         !at(k_pool, 16) || !at(v_pool, 16) || !at(out, 4) || (int64_t)bt->total_q * Hq >= (int64_t)1 << 31)
         return JANUS_ERR_UNSUPPORTED;
     const PrefixPlan plan = prefix_plan(bt->num_seqs, bt->total_q, bt->max_q, bt->max_ctx, bt->total_ctx, prefix_len,
@@ -448,9 +835,9 @@ extern "C" int janus_prefix_attn(const janus_batch *bt, const void *q, int Hq, i
     g.plan = plan;
     hipStream_t st = as_stream(stream);
     if (mla)
-        hipLaunchKernelGGL((prefix_attn<576, 512, true, 32, 3>), dim3(plan.blocks), dim3(PA_THREADS), 0, st, g);
+        hipLaunchKernelGGL(prefix_mla, dim3(plan.blocks), dim3(PA_THREADS), 0, st, g);
     else
-        hipLaunchKernelGGL((prefix_attn<128, 128, false, 64, 2>), dim3(plan.blocks), dim3(PA_THREADS), 0, st, g);
+        hipLaunchKernelGGL(prefix_mqa, dim3(plan.blocks), dim3(PA_THREADS), 0, st, g);
     if (!g.part)
         return launch_status();
     if (hipGetLastError() != hipSuccess)
