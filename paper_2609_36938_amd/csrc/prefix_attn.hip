@@ -19,7 +19,7 @@
 #include "janus_host.hpp"
 #include "launch_rules.hpp"
 
-#include <algorithm>
+#include <type_traits>
 
 namespace janus {
 
@@ -425,11 +425,12 @@ JANUS_DEV void plain_rows(const PrefixArgs &g, const PrefixRange &r, const int *
 }
 
 constexpr int PM_KT = 32, PM_STEPS = 576 / 16;
-constexpr int PM_MAIN = PM_KT * 1024, PM_BUF = PM_MAIN + PM_KT * 128;  // dims 0..511, then 512..575
+constexpr int PM_MAIN = PM_KT * 1024, PM_TAIL = PM_KT * 128;  // bytes of dims 0..511 of a tile, and of 512..575
 // A row's maximum is that of its first tile, and probabilities may exceed 1 by this
 // much (log2): nothing is lost, their exponents have room.  Rows that outgrow it
 // are done again from their maxima, so that O is never rescaled.
 constexpr float PM_HEADROOM = 32.f;
+constexpr int PM_WITH = 16;  // steps of P V among those of K Q^T
 
 // S^T on registers that are not accumulators: O fills all 256 of those, and the
 // compiler would put S among them.  It inserts no wait states for assembly: two
@@ -445,9 +446,12 @@ JANUS_DEV void mfma_next(v16f &s, v4i a, v8bf b)
 }
 JANUS_DEV void settled(v16f &s) { asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s)); }
 
+template <bool SMALL>
 __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
 {
-    __shared__ __attribute__((aligned(16))) uint8_t ring[3 * PM_BUF];
+    // Tile t is scored while tile t - 1 meets its probabilities and two more are on
+    // their way; the last dims are done with a tile earlier.
+    __shared__ __attribute__((aligned(16))) uint8_t main_ring[4 * PM_MAIN], tail_ring[3 * PM_TAIL];
     __shared__ v4i sP[2][PA_WAVES][2][64];       // probabilities of the waves' rows, as operands
     __shared__ v4i sOver;                        // a wave's rows outgrew their maxima
     __shared__ int sLim[PA_ROWS];
@@ -486,39 +490,61 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
         return g.k + (((int64_t)pt[key >> g.page_shift] << g.page_shift) + (key & ps)) * (int64_t)rb32;
     };
     // Wave w gathers rows 8 w .. 8 w + 7: dims 0..511 a row at a time (64 lanes of 16
-    // bytes), the last 64 dims of the eight together.
+    // bytes), the last 64 dims of the eight together.  Keys outside [kbeg, kend) load the nearest
+    // one inside.
     const int tr = lane >> 3;
-    auto issue = [&](int t) {
-        uint8_t *dst = ring + (t % 3) * PM_BUF;
+    auto entry = [&](int t) {  // table entry of the wave's rows of tile t, pages of eight ids and more
+        return pt[min(max(base0 + t * PM_KT + 8 * wave, kbeg), kend - 1) >> g.page_shift];
+    };
+    auto fire = [&](int t, int page, int i) {
         const int key0 = base0 + t * PM_KT + 8 * wave;
-        if (g.page_shift >= 3 && key0 >= kbeg && key0 + 8 <= kend) {
-            const uint8_t *src = key_row(key0);
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                gather16(src + i * (int64_t)rb32, 16u * (lane ^ swz16(8 * (wave & 1) + i)), dst + 1024 * (8 * wave + i));
-            gather16(src, tr * rb32 + 1024u + 16u * ((lane & 7) ^ swz8(8 * (wave & 1) + tr)),
-                     dst + PM_MAIN + 1024 * wave);
+        const uint8_t *first = g.k + ((int64_t)page << g.page_shift) * rb32;
+        int ln = lane;
+        asm volatile("" : "+v"(ln));  // the lane's chunk is worked out here, not kept for the whole loop
+        if (i < 8) {
+            const int key = min(max(key0 + i, kbeg), kend - 1) & ps;
+            gather16(first + (int64_t)key * rb32, 16u * (ln ^ swz16(8 * (wave & 1) + i)),
+                     main_ring + (t & 3) * PM_MAIN + 1024 * (8 * wave + i));
         } else {
-            // keys outside [kbeg, kend) load the nearest one inside
+            const int from = min(max(key0, kbeg), kend - 1), key = min(max(key0 + (ln >> 3), kbeg), kend - 1);
+            gather16(first + (int64_t)(from & ps) * rb32,
+                     (key - from) * rb32 + 1024u + 16u * ((ln & 7) ^ swz8(8 * (wave & 1) + (ln >> 3))),
+                     tail_ring + t % 3 * PM_TAIL + 1024 * wave);
+        }
+    };
+    auto issue = [&](int t) {
+        if constexpr (!SMALL) {
+            const int page = entry(t);
+#pragma unroll
+            for (int i = 0; i < 9; ++i)
+                fire(t, page, i);
+        } else {
+            const int key0 = base0 + t * PM_KT + 8 * wave;
             const uint8_t *mine = g.k;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const uint8_t *src = key_row(min(max(key0 + i, kbeg), kend - 1));
-                gather16(src, 16u * (lane ^ swz16(8 * (wave & 1) + i)), dst + 1024 * (8 * wave + i));
+                gather16(src, 16u * (lane ^ swz16(8 * (wave & 1) + i)),
+                         main_ring + (t & 3) * PM_MAIN + 1024 * (8 * wave + i));
                 mine = tr == i ? src : mine;
             }
-            gather16(mine + 1024 + 16 * ((lane & 7) ^ swz8(8 * (wave & 1) + tr)), dst + PM_MAIN + 1024 * wave);
+            gather16(mine + 1024 + 16 * ((lane & 7) ^ swz8(8 * (wave & 1) + tr)),
+                     tail_ring + t % 3 * PM_TAIL + 1024 * wave);
         }
     };
-    if (nt > 0)
+    // The wave's gathers have landed but for the newest tile's nine.
+    auto landed = [&]() { __builtin_amdgcn_s_waitcnt(vmcnt_only(9)); };
+    if (nt > 0) {
         issue(0);
+        issue(1);
+    }
 
     const int kcol = (hf ^ swz16(c32)) * 16, tcol = (hf ^ swz8(c32)) * 16;
     const int vkey = 4 * hf + ((lane >> 2) & 3);
     const int vch = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
     v16f s;
     v8bf pb[2];
-    __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
+    landed();
     lds_barrier();
     int bmin;  // keys before it are every row's of the block
     {
@@ -532,15 +558,48 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
     }
     int bad = 0;  // a tile where rows end holds values of V that are not finite
 
-    // S^T of tile t; K operands are read AHEAD steps before their MFMA
-    auto logits = [&](int t) {
-        const uint8_t *tile = ring + (t % 3) * PM_BUF;
+    // O += P V of a tile, this wave's dims, as 32 steps: keys 16 h + .., dims 128 wave +
+    // 32 d + .., rows 32 rb + .., with j = 16 h + 4 d + rb.  The operands of step j are read
+    // four steps before it.
+    v4i p[PA_WAVES];
+    v8bf va[2];
+    auto read_v = [&](int t, int h, int d) {
+        const uint8_t *vt = main_ring + (t & 3) * PM_MAIN + 256 * wave;
+        v4s16 part[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int k = 16 * h + 8 * u + vkey;
+            part[u] = lds_read_tr16(vt, k * 1024 + 16 * ((4 * d + vch) ^ swz16(8 * u + vkey)) + 8 * (lane & 1));
+        }
+        __builtin_memcpy(&va[d & 1], part, 16);
+    };
+    auto product_begin = [&](int t) {
+#pragma unroll
+        for (int rb = 0; rb < PA_WAVES; ++rb)
+            p[rb] = sP[t & 1][rb][0][lane];
+        read_v(t, 0, 0);
+    };
+    auto product_step = [&](int t, int j) {
+        const int h = j / 16, d = j / 4 % 4, rb = j % 4;
+        if (rb == 0 && j + 4 < 32)
+            read_v(t, (j + 4) / 16, (j + 4) / 4 % 4);
+        o[d][rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[d & 1], as_v8bf(p[rb]), o[d][rb], 0, 0, 0);
+        if (h == 0 && d == 3)
+            p[rb] = sP[t & 1][rb][1][lane];
+    };
+    // S^T of tile t, with the first `with` steps of the tile before it between its own:
+    // its MFMAs wait for each other.  K operands are read AHEAD steps ahead.
+    auto logits = [&](int t, auto with, int page) {
+        constexpr int WITH = decltype(with)::value;
+        const uint8_t *tile = main_ring + (t & 3) * PM_MAIN, *tail = tail_ring + t % 3 * PM_TAIL;
         constexpr int AHEAD = 4;
         auto kop = [&](int st) {
             return st < 32 ? *(const v4i *)(tile + c32 * 1024 + (kcol ^ (32 * (st & 7))) + 256 * (st >> 3))
-                           : *(const v4i *)(tile + PM_MAIN + c32 * 128 + (tcol ^ (32 * (st & 3))));
+                           : *(const v4i *)(tail + c32 * 128 + (tcol ^ (32 * (st & 3))));
         };
         v4i ahead[AHEAD];
+        if (WITH)
+            product_begin(t - 1);
 #pragma unroll
         for (int x = 0; x < AHEAD; ++x)
             ahead[x] = kop(x);
@@ -552,6 +611,10 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
                 mfma_next(s, ahead[st % AHEAD], qf[st]);
             if (st + AHEAD < PM_STEPS)
                 ahead[st % AHEAD] = kop(st + AHEAD);
+            if (st < WITH)
+                product_step(t - 1, st);
+            if (!SMALL && WITH && st < 9)
+                fire(t + 2, page, st);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -569,7 +632,7 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
             s[i] = key >= kbeg && key < lim ? s[i] * g.scale_log2 : -INFINITY;
         }
         if (!inside) {
-            const uint8_t *tile = ring + (t % 3) * PM_BUF;
+            const uint8_t *tile = main_ring + (t & 3) * PM_MAIN;
 #pragma unroll 2
             for (int w = 0; w < 8; ++w) {
                 const v4i x = *(const v4i *)(tile + 1024 * (4 * w + (lane >> 4)) + 256 * wave + 16 * (lane & 15));
@@ -608,34 +671,8 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
     auto give = [&](int t) {
         sP[t & 1][wave][0][lane] = __builtin_bit_cast(v4i, pb[0]);
         sP[t & 1][wave][1][lane] = __builtin_bit_cast(v4i, pb[1]);
-        __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
+        landed();
         lds_barrier();
-    };
-    // O += P V of tile t, this wave's dims
-    auto product = [&](int t) {
-        const uint8_t *vt = ring + (t % 3) * PM_BUF + 256 * wave;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            v8bf p[PA_WAVES];
-#pragma unroll
-            for (int rb = 0; rb < PA_WAVES; ++rb)
-                p[rb] = as_v8bf(sP[t & 1][rb][h][lane]);
-#pragma unroll
-            for (int d = 0; d < 4; ++d) {
-                // keys 16 h + .., dims 128 wave + 32 d + ..
-                v4s16 part[2];
-                v8bf a;
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const int k = 16 * h + 8 * u + vkey;
-                    part[u] = lds_read_tr16(vt, k * 1024 + 16 * ((4 * d + vch) ^ swz16(8 * u + vkey)) + 8 * (lane & 1));
-                }
-                __builtin_memcpy(&a, part, 16);
-#pragma unroll
-                for (int rb = 0; rb < PA_WAVES; ++rb)
-                    o[d][rb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, p[rb], o[d][rb], 0, 0, 0);
-            }
-        }
     };
     if (nt > 0) {
         // The second time round, the rows' maxima over all their keys are known.
@@ -649,21 +686,38 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
                     for (int i = 0; i < 16; ++i)
                         o[d][rb][i] = 0.f;
             lsum = 0.f;
-            if (nt > 1)
-                issue(1);
-            logits(0);
+            issue(2);
+            logits(0, std::integral_constant<int, 0>{}, 0);
             probabilities(mask(0));
             give(0);
+            int page = SMALL ? 0 : entry(3);
 #pragma unroll 1
             for (int t = 1; t < nt; ++t) {
-                if (t + 1 < nt)
-                    issue(t + 1);
-                logits(t);
+                // (behind the last tile the gathers read its last key again)
+                const int next = SMALL ? 0 : entry(t + 3);
+                if (SMALL)
+                    issue(t + 2);
+                logits(t, std::integral_constant<int, PM_WITH>{}, page);
+                page = next;
+#pragma unroll
+                for (int j = PM_WITH; j < PM_WITH + 4; ++j)
+                    product_step(t - 1, j);
+                __builtin_amdgcn_sched_barrier(0);
                 probabilities(mask(t));
-                product(t - 1);
+#pragma unroll
+                for (int j = PM_WITH + 4; j < 32; ++j)
+                    product_step(t - 1, j);
+#pragma unroll
+                for (int j = PM_WITH + 4; j < 32; ++j) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a matrix instruction
+                    __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);  // under it, six others
+                }
                 give(t);
             }
-            product(nt - 1);
+            product_begin(nt - 1);
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                product_step(nt - 1, j);
             if (lane == 0)
                 ((int *)&sOver)[wave] = 0;
             if (__ballot(over) != 0 && lane == 0)
@@ -673,28 +727,32 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
             if (round || !__builtin_amdgcn_readfirstlane(any[0] | any[1] | any[2] | any[3]))
                 break;
             over = false;
-            issue(0);
             __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
             lds_barrier();
+            issue(0);
+            issue(1);
 #pragma unroll 1
             for (int t = 0; t < nt; ++t) {
-                if (t + 1 < nt)
-                    issue(t + 1);
-                logits(t);
+                landed();
+                lds_barrier();
+                issue(t + 2);
+                logits(t, std::integral_constant<int, 0>{}, 0);
                 const float mult = mask(t);
                 float mx = s[0];
 #pragma unroll
                 for (int i = 1; i < 16; ++i)
                     mx = fmaxf(mx, s[i]);
                 m = fmaxf(m, mx * mult);
-                __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
-                lds_barrier();
             }
             m = fmaxf(m, __shfl_xor(m, 32));
-            issue(0);
             __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
             lds_barrier();
+            issue(0);
+            issue(1);
+            landed();
+            lds_barrier();
         }
+        __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
     }
 
     // Rows that end in a tile whose V holds an infinity or NaN: a probability of 0
@@ -743,40 +801,92 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
 
 // Joins the ranges of a row: with maxima m_s and sums l_s, M = max m_s and w_s =
 // 2^(m_s - M), O = sum w_s O_s / sum w_s l_s and lse = (M + log2 sum w_s l_s) ln 2.
-// Eight dims a lane; a range without keys (l = 0) wrote no O.
-template <int DV>
+// A range without keys (l = 0) wrote no O.  A worker is DV / 8 lanes of eight dims;
+// WPR workers share a row's ranges, so that few rows of many ranges are not a chain of loads.
+template <int DV, int WPR>
 __global__ __launch_bounds__(256) void prefix_combine(const float *__restrict__ part, int slots, int rows,
                                                       const int32_t *__restrict__ q_start, int num_seqs, int heads,
                                                       void *__restrict__ out, int out_f32, float *__restrict__ lse)
 {
-    constexpr int LANES = DV / 8;
-    const int row = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, in = threadIdx.x % LANES;
-    if (row >= q_start[num_seqs] * heads || row >= rows)
-        return;
-    const float2 *ml = (const float2 *)(part + (int64_t)slots * rows * DV) + row;
+    constexpr int LANES = DV / 8, WORKERS = 256 / LANES;
+    static_assert(WORKERS % WPR == 0, "whole rows in a block");
+    __shared__ v4f sO[WPR > 1 ? 2 * 256 : 1];
+    __shared__ float sL[WPR > 1 ? WORKERS : 1];
+    const int worker = threadIdx.x / LANES, in = threadIdx.x % LANES, w = worker % WPR;
+    const int row = blockIdx.x * (WORKERS / WPR) + worker / WPR;
+    const bool live = row < min(rows, q_start[num_seqs] * heads);
+    const float2 *ml = (const float2 *)(part + (int64_t)slots * rows * DV) + (live ? row : 0);
+    const float *po = part + (int64_t)(live ? row : 0) * DV + 8 * in;
+    const int64_t step = (int64_t)rows * DV;
     float M = M_INIT;
-    for (int s = 0; s < slots; ++s) {
+    for (int s = in; s < slots; s += LANES) {
         const float2 x = ml[(int64_t)s * rows];
-        if (x.y != 0.f)
-            M = fmaxf(M, x.x);
+        M = x.y != 0.f ? fmaxf(M, x.x) : M;
     }
+#pragma unroll
+    for (int o = 1; o < LANES; o <<= 1)
+        M = fmaxf(M, __shfl_xor(M, o));
     float L = 0.f;
     v4f a = {0.f, 0.f, 0.f, 0.f}, b = a;
-    for (int s = 0; s < slots; ++s) {
-        const float2 x = ml[(int64_t)s * rows];
-        if (x.y == 0.f)
-            continue;
-        const float w = __builtin_amdgcn_exp2f(x.x - M);
-        const v4f *src = (const v4f *)(part + ((int64_t)s * rows + row) * DV) + 2 * in;
-        L += w * x.y;
-        a += w * src[0];
-        b += w * src[1];
+    for (int s0 = w; s0 < slots; s0 += 4 * WPR) {
+        float2 x[4];
+        v4f u[4], v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int s = s0 + k * WPR;
+            x[k] = s < slots ? ml[(int64_t)s * rows] : float2{0.f, 0.f};
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            u[k] = v[k] = v4f{0.f, 0.f, 0.f, 0.f};
+            if (x[k].y != 0.f) {
+                const v4f *src = (const v4f *)(po + (int64_t)(s0 + k * WPR) * step);
+                u[k] = src[0];
+                v[k] = src[1];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (x[k].y != 0.f) {
+                const float f = __builtin_amdgcn_exp2f(x[k].x - M);
+                L += f * x[k].y;
+                a += f * u[k];
+                b += f * v[k];
+            }
     }
+    if constexpr (WPR > 1) {
+        sO[2 * threadIdx.x] = a;
+        sO[2 * threadIdx.x + 1] = b;
+        if (in == 0)
+            sL[worker] = L;
+        __syncthreads();
+        if (w != 0)
+            return;
+#pragma unroll
+        for (int k = 1; k < WPR; ++k) {
+            a += sO[2 * (threadIdx.x + k * LANES)];
+            b += sO[2 * (threadIdx.x + k * LANES) + 1];
+            L += sL[worker + k];
+        }
+    }
+    if (!live)
+        return;
     const float inv = L != 0.f ? 1.f / L : 0.f;
     store_out4(out, out_f32, (int64_t)row * DV + 8 * in, a * inv);
     store_out4(out, out_f32, (int64_t)row * DV + 8 * in + 4, b * inv);
     if (lse && in == 0)
         lse[row] = L != 0.f ? (M + log2f(L)) * LN2 : -INFINITY;
+}
+
+template <int DV>
+static void launch_combine(const PrefixArgs &g, hipStream_t st)
+{
+    // a worker a row up to four ranges: all of them are in flight at once
+    constexpr int WORKERS = 256 / (DV / 8);
+    const bool one = g.plan.slots <= 4;
+    const auto kernel = one ? &prefix_combine<DV, 1> : &prefix_combine<DV, WORKERS>;
+    hipLaunchKernelGGL(kernel, dim3(one ? ceil_div(g.plan.rows, WORKERS) : g.plan.rows), dim3(256), 0, st, g.part,
+                       g.plan.slots, g.plan.rows, g.q_start, g.num_seqs, g.heads, g.out, g.out_f32, g.lse);
 }
 
 }  // namespace janus
@@ -835,16 +945,16 @@ extern "C" int janus_prefix_attn(const janus_batch *bt, const void *q, int Hq, i
     g.plan = plan;
     hipStream_t st = as_stream(stream);
     if (mla)
-        hipLaunchKernelGGL(prefix_mla, dim3(plan.blocks), dim3(PA_THREADS), 0, st, g);
+        hipLaunchKernelGGL(page_size < 8 ? prefix_mla<true> : prefix_mla<false>, dim3(plan.blocks), dim3(PA_THREADS), 0, st, g);
     else
         hipLaunchKernelGGL(prefix_mqa, dim3(plan.blocks), dim3(PA_THREADS), 0, st, g);
     if (!g.part)
         return launch_status();
     if (hipGetLastError() != hipSuccess)
         return JANUS_ERR_DEVICE;
-    const int lanes = dv / 8;
-    hipLaunchKernelGGL(mla ? prefix_combine<512> : prefix_combine<128>, dim3(ceil_div(plan.rows, 256 / lanes)),
-                       dim3(256), 0, st, g.part, plan.slots, plan.rows, bt->q_start, bt->num_seqs, Hq, out, g.out_f32,
-                       lse);
+    if (mla)
+        launch_combine<512>(g, st);
+    else
+        launch_combine<128>(g, st);
     return launch_status();
 }
