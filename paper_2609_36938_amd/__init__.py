@@ -364,35 +364,43 @@ _LAYOUTS = {"half": 0, "interleaved": 1}
 _SCALINGS = {None: 0, "linear": 1, "yarn": 2}
 
 
-def _device(what: str, *tensors) -> torch.device:
-    """The one device that all the tensors (None: absent) are on."""
-    dev = None
+def _device(what: str, *tensors) -> int:
+    """Index of the one GPU that all the tensors (None: absent) are on."""
+    dev = -1
     for t in tensors:
-        if t is None:
-            continue
-        if not t.is_cuda or (dev is not None and t.device != dev):
-            raise JanusError(f"{what}: tensors of one GPU expected")
-        dev = t.device
+        if t is not None:
+            d = t.get_device()  # -1 on the host
+            if d < 0 or (d != dev and dev >= 0):
+                raise JanusError(f"{what}: tensors of one GPU expected")
+            dev = d
     return dev
 
 
 def _want(what: str, name: str, t, dtype, *shape):
     """t has this dtype, these sizes (None: any) and adjacent elements."""
-    if t.dtype != dtype or t.dim() != len(shape) or not t.is_contiguous() or any(
-            n is not None and n != m for n, m in zip(shape, t.shape)):
+    have = t.shape
+    if t.dtype is not dtype or not t.is_contiguous() or (have != shape and (
+            len(have) != len(shape) or any(n is not None and n != m for n, m in zip(shape, have)))):
         raise JanusError(f"{what}: {name} is to be a contiguous {dtype} tensor of shape "
-                         f"{tuple('any' if n is None else n for n in shape)}, not {t.dtype} {tuple(t.shape)}")
+                         f"{tuple('any' if n is None else n for n in shape)}, not {t.dtype} {tuple(have)}")
 
 
-def _launch(what: str, dev: torch.device, stream, fn, *args):
-    """fn(*args, stream) on dev, whatever device is current."""
-    s = torch.cuda.current_stream(dev) if stream is None else stream
-    if torch.cuda.current_device() == dev.index:
-        rc = fn(*args, ctypes.c_void_p(s.cuda_stream))
+def _at(t: Optional[torch.Tensor]):
+    """Address of a tensor that _device has seen."""
+    return None if t is None else t.data_ptr()
+
+
+def _launch(what: str, dev: int, stream, fn, *args):
+    """fn(*args, stream) on GPU dev, whatever device is current.  (The raw stream: the object around it
+    takes as long as the launch.)"""
+    s = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+    if torch.cuda.current_device() == dev:
+        rc = fn(*args, s)
     else:
         with torch.cuda.device(dev):
-            rc = fn(*args, ctypes.c_void_p(s.cuda_stream))
-    _check(rc, what)
+            rc = fn(*args, s)
+    if rc != 0:
+        _check(rc, what)
 
 
 def rotary_frequencies(dim: int, base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0,
@@ -459,21 +467,22 @@ def page_grow(batch: Batch, page_size: int, free_list, page_table, free_head=Non
     pages taken, the next free_head, pages short); out = (slots, counts) to
     write those tensors."""
     what = "janus_page_grow"
-    if out is None:
-        out = (torch.empty(batch.total_q, dtype=torch.int64, device=page_table.device),
-               torch.empty(3, dtype=torch.int32, device=page_table.device))
-    slots, counts = out
-    dev = _device(what, page_table, free_list, free_head, slots, counts, batch.q_start)
     _want(what, "page_table", page_table, torch.int32, batch.c.num_seqs, None)
     _want(what, "free_list", free_list, torch.int32, None)
-    _want(what, "slots", slots, torch.int64, batch.total_q)
-    _want(what, "counts", counts, torch.int32, 3)
+    if out is None:
+        slots = torch.empty(batch.total_q, dtype=torch.int64, device=page_table.device)
+        counts = torch.empty(3, dtype=torch.int32, device=page_table.device)
+    else:
+        slots, counts = out
+        _want(what, "slots", slots, torch.int64, batch.total_q)
+        _want(what, "counts", counts, torch.int32, 3)
+    dev = _device(what, page_table, free_list, free_head, slots, counts, batch.q_start)
     if free_head is not None and (free_head.dtype != torch.int32 or free_head.numel() != 1):
         raise JanusError(f"{what}: free_head is to be one int32")
-    # an empty tensor has no address
-    _launch(what, dev, stream, lib().janus_page_grow, batch.ref, int(page_size), _ptr(free_list),
-            int(free_list.numel()), _ptr(free_head), _ptr(page_table), _table(batch, page_table, page_size),
-            _ptr(slots) if batch.total_q else _ptr(counts), _ptr(counts))
+    # (an empty tensor has no address)
+    _launch(what, dev, stream, lib().janus_page_grow, batch.ref, int(page_size), _at(free_list),
+            int(free_list.numel()), _at(free_head), _at(page_table), _table(batch, page_table, page_size),
+            _at(slots) if batch.total_q else _at(counts), _at(counts))
     return page_table, slots, counts
 
 
@@ -520,8 +529,8 @@ def rope(batch: Batch, rotary: Rotary, x, out=None, out_dtype: Optional[str] = N
     rotary._check(what, batch)
     dev = _device(what, x, out, out_scale, batch.q_start, rotary.inv_freq)
     if batch.total_q:
-        _launch(what, dev, stream, lib().janus_rope, batch.ref, rotary.ref, _ptr(x), xdt, x.stride(0), x.stride(1),
-                int(x.shape[1]), int(x.shape[2]), _ptr(out), odt, out.stride(0), out.stride(1), _ptr(out_scale))
+        _launch(what, dev, stream, lib().janus_rope, batch.ref, rotary.ref, _at(x), xdt, x.stride(0), x.stride(1),
+                int(x.shape[1]), int(x.shape[2]), _at(out), odt, out.stride(0), out.stride(1), _at(out_scale))
     return out, out_scale
 
 
@@ -563,9 +572,9 @@ def kv_append(batch: Batch, x, out, rotary: Optional[Rotary] = None, x_rot=None,
         rotary._check(what, batch)
     dev = _device(what, out, x, x_rot, rows, out_scale, batch.q_start, None if rotary is None else rotary.inv_freq)
     if batch.total_q:
-        _launch(what, dev, stream, lib().janus_kv_append, batch.ref, None if rotary is None else rotary.ref, _ptr(x),
-                xdt, 0 if x is None else x.stride(0), _ptr(x_rot), 0 if x_rot is None else x_rot.stride(0), n,
-                _ptr(rows), num_rows, _ptr(out), odt, int(out.shape[-1]) * out.element_size(), _ptr(out_scale))
+        _launch(what, dev, stream, lib().janus_kv_append, batch.ref, None if rotary is None else rotary.ref, _at(x),
+                xdt, 0 if x is None else x.stride(0), _at(x_rot), 0 if x_rot is None else x_rot.stride(0), n,
+                _at(rows), num_rows, _at(out), odt, int(out.shape[-1]) * out.element_size(), _at(out_scale))
     return out
 
 
@@ -597,13 +606,13 @@ def prefix_attn(batch: Batch, q, k_pool, v_pool, page_table, page_size: int, pre
     dev = _device(what, q, k_pool, v_pool, page_table, out, lse, workspace, batch.q_start)
     if batch.total_q == 0:
         return out, lse
-    args = (batch.ref, _ptr(q), Hq, dqk, dv, _ptr(k_pool), _ptr(v_pool), krs, vrs, _ptr(page_table),
-            _table(batch, page_table, page_size), int(page_size), int(prefix_len), float(scale), _ptr(out), odt[0],
-            _ptr(lse))
+    args = (batch.ref, _at(q), Hq, dqk, dv, _at(k_pool), _at(v_pool), krs, vrs, _at(page_table),
+            _table(batch, page_table, page_size), int(page_size), int(prefix_len), float(scale), _at(out), odt[0],
+            _at(lse))
     need = ctypes.c_size_t(0)
     _launch(what, dev, stream, lib().janus_prefix_attn, *args, None, ctypes.byref(need))
     if workspace is None:
         workspace = torch.empty(max(int(need.value), 1), dtype=torch.uint8, device=q.device)
     have = ctypes.c_size_t(workspace.numel() * workspace.element_size())
-    _launch(what, dev, stream, lib().janus_prefix_attn, *args, _ptr(workspace), ctypes.byref(have))
+    _launch(what, dev, stream, lib().janus_prefix_attn, *args, _at(workspace), ctypes.byref(have))
     return out, lse

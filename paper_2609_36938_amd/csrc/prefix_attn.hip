@@ -112,22 +112,23 @@ JANUS_DEV void split_odd(int x, int &fin, int &up, int &down)
 JANUS_DEV int swz16(int r) { return ((r & 1) << 3) | ((r & 2) << 1) | ((r & 4) >> 1) | ((r & 8) >> 3); }
 JANUS_DEV int swz8(int r) { return ((r & 2) << 1) | ((r & 4) >> 1) | ((r & 8) >> 3); }
 
-constexpr int PQ_KT = 64;  // keys of a tile
+constexpr int PQ_KT = 32;  // keys of a tile
 
-__global__ __launch_bounds__(PA_THREADS, 1) void prefix_mqa(PrefixArgs g)
+__global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
 {
-    constexpr int RB = 256, CH = 16;                     // bytes and chunks of a row
+    constexpr int RB = 256;                              // bytes of a row
     constexpr int KBUF = PQ_KT * RB, BUF = 2 * KBUF;     // K rows, then V rows
     constexpr int STEPS = 8, NB = 4, NK = PQ_KT / 32;    // K-steps, blocks of 32 dims and of 32 keys
     constexpr int GATHERS = KBUF / (1024 * PA_WAVES);    // a wave's, of each pool
-    __shared__ __attribute__((aligned(16))) uint8_t ring[2 * BUF];
+    __shared__ __attribute__((aligned(16))) uint8_t ring[3 * BUF];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c32 = lane & 31, hf = lane >> 5;
     const PrefixRange r = prefix_range(g, blockIdx.x);
     if (r.row0 >= r.row1)
         return;
-    const int32_t *pt = g.table + (int64_t)r.sess * g.pt_ld;
+    typedef const __attribute__((address_space(4))) int32_t *scalar_i32;  // read through the scalar cache
+    const scalar_i32 pt = (scalar_i32)(g.table + (int64_t)r.sess * g.pt_ld);
     const int kbeg = r.kbeg, kend = r.kend;
     const int row = r.row0 + 32 * wave + c32;
     const bool live = row < r.row1;
@@ -154,42 +155,54 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mqa(PrefixArgs g)
     float m = M_INIT, lsum = 0.f;
 
     // Tiles begin at multiples of their length: a tile of longer pages lies in one.
-    // Keys outside [kbeg, kend) load the nearest one inside.
+    // A wave gathers four rows at a time, rows 16 j + 4 wave .. of K and of V.
     const int base0 = kbeg & ~(PQ_KT - 1);
     const int nt = kend > kbeg ? (kend - base0 + PQ_KT - 1) / PQ_KT : 0;
-    const bool one_page = (1 << g.page_shift) >= PQ_KT;
-    auto slot_of = [&](int key) {
-        return ((int64_t)pt[key >> g.page_shift] << g.page_shift) + (key & ((1 << g.page_shift) - 1));
-    };
-    auto issue = [&](int t) {
-        uint8_t *dst = ring + (t & 1) * BUF;
+    const int ps = (1 << g.page_shift) - 1;
+    const int gr = lane >> 4;
+    const uint32_t gc = 16 * ((lane & 15) ^ swz16(4 * wave + gr));
+    const uint32_t koff = gr * (uint32_t)g.k_rb + gc, voff = gr * (uint32_t)g.v_rb + gc;
+    auto entry = [&](int t) { return pt[min(base0 + t * PQ_KT, kend - 1) >> g.page_shift]; };
+    auto issue = [&](int t, int page) {
+        uint8_t *dst = ring + t % 3 * BUF + 1024 * wave;
         const int base = base0 + t * PQ_KT;
-        const int first = max(kbeg - base, 0), last = min(kend - base, PQ_KT) - 1;
-        const int64_t slot0 = one_page ? slot_of(base) : 0;
+        if (ps >= PQ_KT - 1 && base >= kbeg && base + PQ_KT <= kend) {
+            const int64_t slot = ((int64_t)page << g.page_shift) + (base & ps) + 4 * wave;
 #pragma unroll
-        for (int j = 0; j < 2 * GATHERS; ++j) {
-            const bool isv = j >= GATHERS;
-            const int at = 64 * (wave + PA_WAVES * (isv ? j - GATHERS : j));
-            const int k = (at + lane) / CH, c = (at + lane) % CH;
-            const int kk = min(max(k, first), last);
-            const int64_t slot = one_page ? slot0 + kk : slot_of(base + kk);
-            const uint8_t *src = (isv ? g.v : g.k) + slot * (isv ? g.v_rb : g.k_rb) + 16 * (c ^ swz16(k));
-            gather16(src, dst + (isv ? KBUF : 0) + 16 * at);
+            for (int j = 0; j < GATHERS; ++j) {
+                gather16(g.k + (slot + 16 * j) * g.k_rb, koff, dst + 4096 * j);
+                gather16(g.v + (slot + 16 * j) * g.v_rb, voff, dst + KBUF + 4096 * j);
+            }
+        } else {
+            // keys outside [kbeg, kend) load the nearest one inside
+#pragma unroll
+            for (int j = 0; j < GATHERS; ++j) {
+                const int key = min(max(base + 16 * j + 4 * wave + gr, kbeg), kend - 1);
+                const int64_t slot = ((int64_t)pt[key >> g.page_shift] << g.page_shift) + (key & ps);
+                gather16(g.k + slot * g.k_rb + gc, dst + 4096 * j);
+                gather16(g.v + slot * g.v_rb + gc, dst + KBUF + 4096 * j);
+            }
         }
     };
-    if (nt > 0)
-        issue(0);
+    if (nt > 0) {
+        issue(0, entry(0));
+        issue(1, entry(1));
+    }
+    int page = nt > 0 ? entry(2) : 0;
 
     const int kcol = (hf ^ swz16(c32)) * 16;  // K: chunk 2 st + hf of key c32
     // V: this lane addresses key 16 s + 8 u + 4 hf + (lane / 4) % 4 and dims 32 d + 16 (lane / 16 % 2) + 4 (lane % 4)
     const int vkey = 4 * hf + ((lane >> 2) & 3);
     const int vch = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
     for (int t = 0; t < nt; ++t) {
-        __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
+        // tile t has landed, the next one's gathers may be on their way (behind the last
+        // tile they read its last key again)
+        __builtin_amdgcn_s_waitcnt(vmcnt_only(2 * GATHERS));
         lds_barrier();
-        if (t + 1 < nt)
-            issue(t + 1);
-        const uint8_t *tile = ring + (t & 1) * BUF, *vt = tile + KBUF;
+        const int next = entry(t + 3);
+        issue(t + 2, page);
+        page = next;
+        const uint8_t *tile = ring + t % 3 * BUF, *vt = tile + KBUF;
         const int base = base0 + t * PQ_KT;
 
         // K operands are read AHEAD steps before their MFMA, with a scheduling
@@ -337,7 +350,8 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mqa(PrefixArgs g)
         }
     }
 
-    float l = lsum + __shfl_xor(lsum, 32);
+    __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
+    const float l = lsum + __shfl_xor(lsum, 32);
     if (!live)
         return;
     if (g.part) {

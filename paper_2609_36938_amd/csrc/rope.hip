@@ -44,6 +44,7 @@ struct RopeArgs {
     uint8_t *out;
     int64_t o_rs, o_hs;          // bytes
     int plain_units;             // units a head of the elements that are only copied (0: in place)
+    int per_shift;               // log2 of a head's units, or -1
     int scatter;                 // cache rows: to `rows`, or by context where it is null
     const int64_t *rows;
     int64_t num_rows;
@@ -63,36 +64,46 @@ JANUS_DEV int session_of_row_lanes(const int32_t *q_start, int num_seqs, int row
         uint64_t below = __ballot(s < hi && q_start[s] <= row);
         if constexpr (K < kWave)
             below = (below >> (lane & ~(K - 1))) & ((1ull << K) - 1);
-        lo += max(__popcll(below) - 1, 0) * step;
+        lo += max((int)__popcll(below) - 1, 0) * step;
         hi = min(hi, lo + step);
     }
     return lo;
 }
 
+// V elements as they are loaded, and as fp32.
 template <class T, int V>
-JANUS_DEV void load_group(const T *p, float (&v)[V])
-{
-    if constexpr (V == 1) {
-        if constexpr (std::is_same<T, float>::value)
-            v[0] = *p;
-        else
-            v[0] = bf16_to_f32(*p);
-    } else if constexpr (std::is_same<T, float>::value) {
-        const v4f a = ((const v4f *)p)[0], b = ((const v4f *)p)[1];
+struct Raw {
+    using Word = typename std::conditional<V == 1, T, v4i>::type;
+    static constexpr int N = V * sizeof(T) / sizeof(Word);
+    Word w[N];
+    JANUS_DEV void load(const T *p)
+    {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            v[e] = a[e];
-            v[4 + e] = b[e];
-        }
-    } else {
-        const v4i a = *(const v4i *)p;
+        for (int i = 0; i < N; ++i)
+            w[i] = ((const Word *)p)[i];
+    }
+    JANUS_DEV void unpack(float (&v)[V]) const
+    {
+        if constexpr (V == 1) {
+            if constexpr (sizeof(T) == 4)
+                v[0] = w[0];
+            else
+                v[0] = bf16_to_f32(w[0]);
+        } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            v[2 * e] = __uint_as_float((uint32_t)a[e] << 16);
-            v[2 * e + 1] = __uint_as_float((uint32_t)a[e] & 0xffff0000u);
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if constexpr (sizeof(T) == 4) {
+                        v[4 * i + e] = __int_as_float(w[i][e]);
+                    } else {
+                        v[2 * e] = __uint_as_float((uint32_t)w[i][e] << 16);
+                        v[2 * e + 1] = __uint_as_float((uint32_t)w[i][e] & 0xffff0000u);
+                    }
+                }
         }
     }
-}
+};
 
 // To the nearest bf16, ties to even (NaN stays NaN).
 JANUS_DEV uint32_t bf16_pair(float a, float b)
@@ -144,20 +155,15 @@ JANUS_DEV Unit unit_at(const RopeArgs &g, int u)
 {
     const int turned = g.dim / (2 * V), per = turned + g.plain_units;
     Unit at;
-    at.head = u / per;
+    at.head = g.heads == 1 ? 0 : g.per_shift >= 0 ? u >> g.per_shift : u / per;
     const int r = u - at.head * per;
-    if (r < turned) {
-        at.pair = r * V;
-        at.a = g.off + (g.halves ? r * V : 2 * r * V);
-        at.b = at.a + (g.halves ? g.dim / 2 : V);
-    } else {
-        const int e = 2 * V * (r - turned);  // among the plain elements
-        at.pair = -1;
-        at.a = e < g.off ? e : e + g.dim;
-        at.b = e + V < g.off ? e + V : e + V + g.dim;
-        if (at.b >= g.size)
-            at.b = -1;
-    }
+    const bool turns = r < turned;
+    const int e = 2 * V * (r - turned);  // among the plain elements
+    const int pa = e < g.off ? e : e + g.dim, pb = e + V < g.off ? e + V : e + V + g.dim;
+    const int ta = g.off + (g.halves ? r * V : 2 * r * V);
+    at.pair = turns ? r * V : -1;
+    at.a = turns ? ta : pa;
+    at.b = turns ? ta + (g.halves ? g.dim / 2 : V) : pb < g.size ? pb : -1;
     return at;
 }
 
@@ -166,54 +172,48 @@ __global__ __launch_bounds__(ROPE_THREADS) void rope_rows(RopeArgs g)
 {
     extern __shared__ float2 turn[];  // [rows of the block][dim / 2]: cosine, sine
     __shared__ float red[ROPE_THREADS / kWave];
-    __shared__ int sPos[ROPE_THREADS / LPR];
     constexpr int ROWS = ROPE_THREADS / LPR;
     constexpr bool FP8 = DT == JANUS_FP8_E4M3;
     const int tid = threadIdx.x, lane = tid % LPR, mine = tid / LPR;
-    const int row = blockIdx.x * ROWS + mine;
-    const bool live = row < g.total_q;
+    const bool live = (int64_t)blockIdx.x * ROWS + mine < g.total_q;
+    const int row = live ? blockIdx.x * ROWS + mine : g.total_q - 1;
     const int pairs = g.dim / 2;
     const int units = g.heads * (g.dim / (2 * V) + g.plain_units);
     // fp8 rows: all units of the token, LPR * ROPE_UPT at a time; others: the block's share of them
     const int u0 = FP8 ? 0 : blockIdx.y * LPR * ROPE_UPT;
 
-    float va[ROPE_UPT][V], vb[ROPE_UPT][V];
+    // Loads without a branch, so that all of them are under way at once: lanes
+    // behind the last unit take it again, units of one group take that twice.
+    Unit at[ROPE_UPT];
+    Raw<T, V> ra[ROPE_UPT], rb[ROPE_UPT];
     auto load = [&](int first) {
+        const T *x = (const T *)g.x + (int64_t)row * g.x_rs;
+        const T *xr = g.xr ? (const T *)g.xr + (int64_t)row * g.xr_rs - g.off : nullptr;
+        const int skip = g.xr ? g.dim : 0;  // the rotated elements are elsewhere
 #pragma unroll
         for (int k = 0; k < ROPE_UPT; ++k) {
-            const int u = first + k * LPR + lane;
-#pragma unroll
-            for (int e = 0; e < V; ++e)
-                va[k][e] = vb[k][e] = 0.f;
-            if (!live || u >= units)
-                continue;
-            const Unit at = unit_at<V>(g, u);
-            if (at.pair >= 0 && g.xr) {
-                const T *p = (const T *)g.xr + (int64_t)row * g.xr_rs - g.off;
-                load_group<T, V>(p + at.a, va[k]);
-                load_group<T, V>(p + at.b, vb[k]);
-            } else {
-                const T *p = (const T *)g.x + (int64_t)row * g.x_rs + (int64_t)at.head * g.x_hs;
-                const int skip = g.xr ? g.dim : 0;  // the rotated elements are elsewhere
-                load_group<T, V>(p + (at.a < g.off ? at.a : at.a - skip), va[k]);
-                if (at.b >= 0)
-                    load_group<T, V>(p + (at.b < g.off ? at.b : at.b - skip), vb[k]);
-            }
+            at[k] = unit_at<V>(g, min(first + k * LPR + lane, units - 1));
+            const int a = at[k].a, b = at[k].b < 0 ? a : at[k].b;
+            const bool other = at[k].pair >= 0 && g.xr;
+            const T *p = other ? xr : x + (int64_t)at[k].head * g.x_hs;
+            ra[k].load(p + (other || a < g.off ? a : a - skip));
+            rb[k].load(p + (other || b < g.off ? b : b - skip));
         }
     };
     load(u0);
+    const double freq = pairs > 0 ? g.inv_freq[min(lane, pairs - 1)] : 0.0;
 
     // the token's session, position and output row
     int64_t to = row;
     bool store = live && row < g.q_start[g.num_seqs];
+    int pos;
     {
-        const int b = session_of_row_lanes<LPR>(g.q_start, g.num_seqs, live ? row : 0);
+        const int b = session_of_row_lanes<LPR>(g.q_start, g.num_seqs, row);
         const int tokens = g.hist_len[b] + row - g.q_start[b] + 1;
-        if (lane == 0)
-            sPos[mine] = live && g.positions ? g.positions[row] : tokens - 1;
+        pos = g.positions ? g.positions[row] : tokens - 1;
         if (g.scatter) {
             if (g.rows) {
-                to = live ? g.rows[row] : -1;
+                to = g.rows[row];
             } else {
                 to = (int64_t)g.ctx_start[b] + entries_of(tokens, g.es) - 1;
                 store = store && (tokens & ((1 << g.es) - 1)) == 0;
@@ -221,26 +221,27 @@ __global__ __launch_bounds__(ROPE_THREADS) void rope_rows(RopeArgs g)
             store = store && to >= 0 && to < g.num_rows;
         }
     }
-    __syncthreads();
-    for (int i = tid; i < ROWS * pairs; i += ROPE_THREADS) {
-        const int r = i / pairs, p = i - r * pairs;
-        double t = (double)sPos[r] * g.inv_freq[p] * 0.15915494309189533577;  // turns
+    for (int p = lane; p < pairs; p += LPR) {
+        double t = (double)pos * (p < LPR ? freq : g.inv_freq[p]) * 0.15915494309189533577;  // turns
         t -= rint(t);
         float s, c;
         sincospif(2.f * (float)t, &s, &c);
-        turn[i] = float2{c * g.mag, (g.inverse ? -s : s) * g.mag};
+        turn[mine * pairs + p] = float2{c * g.mag, (g.inverse ? -s : s) * g.mag};
     }
-    __syncthreads();
-    auto rotate = [&](int first) {
+    if constexpr (LPR > kWave)
+        __syncthreads();
+    else
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // (a token is one wave's or less)
+
+    float va[ROPE_UPT][V], vb[ROPE_UPT][V];
+    auto rotate = [&]() {
 #pragma unroll
         for (int k = 0; k < ROPE_UPT; ++k) {
-            const int u = first + k * LPR + lane;
-            if (u >= units)
+            ra[k].unpack(va[k]);
+            rb[k].unpack(vb[k]);
+            if (at[k].pair < 0)
                 continue;
-            const Unit at = unit_at<V>(g, u);
-            if (at.pair < 0)
-                continue;
-            const float2 *t = turn + mine * pairs + at.pair;
+            const float2 *t = turn + mine * pairs + at[k].pair;
             if (g.halves || V == 1) {
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
@@ -265,17 +266,15 @@ __global__ __launch_bounds__(ROPE_THREADS) void rope_rows(RopeArgs g)
     auto put = [&](int first, float inv) {
 #pragma unroll
         for (int k = 0; k < ROPE_UPT; ++k) {
-            const int u = first + k * LPR + lane;
-            if (u >= units || !store)
+            if (first + k * LPR + lane >= units || !store)
                 continue;
-            const Unit at = unit_at<V>(g, u);
-            uint8_t *p = g.out + to * g.o_rs + (int64_t)at.head * g.o_hs;
-            store_group<DT, V>(p + (int64_t)at.a * BYTES, va[k], inv);
-            if (at.b >= 0)
-                store_group<DT, V>(p + (int64_t)at.b * BYTES, vb[k], inv);
+            uint8_t *p = g.out + to * g.o_rs + (int64_t)at[k].head * g.o_hs;
+            store_group<DT, V>(p + (int64_t)at[k].a * BYTES, va[k], inv);
+            if (at[k].b >= 0)
+                store_group<DT, V>(p + (int64_t)at[k].b * BYTES, vb[k], inv);
         }
     };
-    rotate(u0);
+    rotate();
     if constexpr (!FP8) {
         put(u0, 1.f);
     } else {
@@ -295,7 +294,7 @@ __global__ __launch_bounds__(ROPE_THREADS) void rope_rows(RopeArgs g)
         const bool again = units > LPR * ROPE_UPT;
         for (int u = LPR * ROPE_UPT; u < units; u += LPR * ROPE_UPT) {
             load(u);
-            rotate(u);
+            rotate();
             tops();
         }
 #pragma unroll
@@ -312,7 +311,7 @@ __global__ __launch_bounds__(ROPE_THREADS) void rope_rows(RopeArgs g)
             // a row longer than the lanes' registers is read again
             for (int u = 0; u < units; u += LPR * ROPE_UPT) {
                 load(u);
-                rotate(u);
+                rotate();
                 put(u, inv);
             }
         } else {
@@ -328,16 +327,16 @@ __global__ __launch_bounds__(ROPE_THREADS) void rope_rows(RopeArgs g)
 }
 
 template <class T, int DT, int V>
-static void launch_rope_rows(const RopeArgs &g, hipStream_t st)
+static void launch_rope_rows(RopeArgs g, hipStream_t st)
 {
-    const int units = g.heads * (g.dim / (2 * V) + g.plain_units);
-    const int most = DT == JANUS_FP8_E4M3 ? 1 : 65535;
+    const int per = g.dim / (2 * V) + g.plain_units, units = g.heads * per;
+    g.per_shift = pow2(per) ? __builtin_ctz((unsigned)per) : -1;
     auto go = [&](auto lanes) {
         constexpr int LPR = decltype(lanes)::value;
         const int rows = ROPE_THREADS / LPR;
         hipLaunchKernelGGL((rope_rows<T, DT, V, LPR>),
                            dim3(ceil_div(g.total_q, rows),
-                                most == 1 ? 1 : ceil_div(units, LPR * ROPE_UPT)),
+                                DT == JANUS_FP8_E4M3 ? 1 : ceil_div(units, LPR * ROPE_UPT)),
                            dim3(ROPE_THREADS), (size_t)rows * (g.dim / 2) * sizeof(float2), st, g);
     };
     if (units <= 16 * ROPE_UPT)
