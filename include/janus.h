@@ -525,8 +525,8 @@ int janus_kv_append(const janus_batch *b, const janus_rotary *r, const void *x, 
  *   workspace, workspace_bytes: as janus_sparse_attn_split
  * Shapes: MLA (dqk = 576, dv = 512, v_pool == k_pool, equal strides) and MQA
  * (dqk = dv = 128), each with 1 <= Hq <= 128, q and pools 16-byte aligned and
- * row strides in multiples of 8 up to 2^24, total_q * Hq < 2^31; else
- * JANUS_ERR_UNSUPPORTED.  A workspace that is used must be 16-byte aligned, and out 4-byte aligned (else
+ * row strides in multiples of 8 up to 2^24, total_q * Hq + 128 B < 2^31 and
+ * fewer than 2^24 blocks of 128 rows; else JANUS_ERR_UNSUPPORTED.  A workspace that is used must be 16-byte aligned, and out 4-byte aligned (else
  * JANUS_ERR_UNSUPPORTED).  A token with no candidate gets out = 0 and lse = -inf.  Rows from
  * q_start[B] on are left as they are.  Ids that a token does not attend to
  * do not touch its result, whatever their rows hold.

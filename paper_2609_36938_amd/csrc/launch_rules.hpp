@@ -169,6 +169,7 @@ constexpr bool mqa_shared(int64_t total_q, int64_t k)
 constexpr int PA_ROWS = 128;  // (token, head) rows of a block
 constexpr int PA_XCD = 8;
 constexpr int PA_CUS = 256;
+constexpr int64_t PA_MAX_BLOCKS = (1 << 24) - 1;  // a launch takes fewer than 2^32 threads
 
 // First tile of session s's own rows, whose tokens start at q_start: each session has as
 // many tiles as its rows fill, or one more, and none needs the sessions before
@@ -179,44 +180,60 @@ constexpr int prefix_tile_first(int q_start, int heads, int s)
 }
 
 struct PrefixPlan {
-    int rows;          // total_q * heads
     int prefix;        // ids that rows of different sessions meet together
     int chunk;         // keys of a block
     int shared_tiles, shared_chunks;  // over the prefix
     int own_tiles, own_chunks;        // over the ids behind it
+    int whole;         // own tiles, the first ones, that are one block each over all their keys
     int alike;         // own chunks that read the same pages in every session
-    int slots;         // ranges of a row
+    int slots;         // ranges of a row whose keys are split (1: none is)
+    int64_t part_rows;  // rows of each slot in the workspace
     int64_t blocks;
 };
 
-constexpr PrefixPlan prefix_plan(int num_seqs, int total_q, int max_q, int max_ctx, int64_t total_ctx, int prefix_len,
-                                 int heads, bool mla)
+constexpr PrefixPlan prefix_plan(int num_seqs, int total_q, int max_ctx, int64_t total_ctx, int prefix_len, int heads,
+                                 bool mla)
 {
     PrefixPlan p = {};
-    (void)max_q;
-    p.rows = total_q * heads;
-    const int full = (p.rows + PA_ROWS - 1) / PA_ROWS;  // tiles of all rows together
+    const int64_t rows = (int64_t)total_q * heads;
+    const int full = (int)((rows + PA_ROWS - 1) / PA_ROWS);  // tiles of all rows together
     // tiles of the sessions apart, at the mean length
-    const int64_t each = ((int64_t)p.rows / num_seqs + PA_ROWS - 1) / PA_ROWS;
+    const int64_t each = (rows / num_seqs + PA_ROWS - 1) / PA_ROWS;
     const int64_t apart = num_seqs * (each > 1 ? each : 1);
     const bool share = prefix_len > 0 && (int64_t)full * 8 <= apart * 7;
+    const int tile = 32, resident = PA_CUS * (mla ? 1 : 2);
     p.prefix = share ? prefix_len : 0;
     p.shared_tiles = share ? full : 0;
     p.own_tiles = prefix_tile_first(total_q, heads, num_seqs);
+    // Whole rounds of blocks need no split; the last tiles are split over the round that is left.
+    const int64_t rounds = share ? 0 : apart / resident;
+    p.whole = (int)(rounds * resident * p.own_tiles / apart);
+    const int64_t rest = apart - rounds * resident, ids = p.own_tiles - p.whole;
     const int own = max_ctx - p.prefix;
     const int64_t mean = total_ctx / num_seqs > p.prefix ? total_ctx / num_seqs - p.prefix : 0;
     const int span = own > p.prefix ? own : p.prefix;
-    const int tile = mla ? 32 : 64, resident = PA_CUS * (mla ? 1 : 2);
-    // a block's start, and moving a row's range out and in again, in keys
-    const int start = mla ? 128 : 256;
+    // Time of a split, in keys of a block: one round of blocks takes as long as its
+    // longest, more of them share the chip and leave a part of a block at the end.  Each
+    // block starts for `start` keys, and a range of a row costs `join` to write and read again.
+    // Fitted to 18 batches of 1 to 64 sessions, each with 28 chunk lengths (MLA: the chunk
+    // taken is 0.3% off the best one in the mean, MQA 3%; with time by whole
+    // rounds alone it was 6 and 13%).
+    const double start = 16, join = mla ? 0.006 : 0.02;
     double best = -1.0;
     for (int n = 1; n <= 256; n += 1 + n / 16) {
         const int chunk = (span > n ? (span + n - 1) / n + tile - 1 : tile) / tile * tile;
         const int sc = share ? (prefix_len + chunk - 1) / chunk : 0, oc = own > 0 ? (own + chunk - 1) / chunk : 1;
-        const int64_t work = (int64_t)p.shared_tiles * sc + apart * ((mean + chunk - 1) / chunk);
-        const int64_t rounds = (work + resident - 1) / resident;
-        const double cost = (double)rounds * (chunk + start) +
-                            (sc + oc > 1 ? (double)(sc + oc) * p.rows * (mla ? 0.02 : 0.01) + start : 0.0);
+        const int64_t mine = mean > 0 ? (mean + chunk - 1) / chunk : 1;
+        const int64_t together = (int64_t)p.shared_tiles * sc, work = together + rest * mine;
+        const double longest = chunk + start;
+        double cost = longest;
+        if (together + ids * oc > resident && (double)work > (mla ? 0.85 : 1.0) * resident) {
+            const double all = (double)together * longest + (double)rest * ((double)mean + (double)mine * start);
+            const double shared_out = all / resident + 0.3 * longest;
+            cost = shared_out > longest ? shared_out : longest;
+        }
+        if (sc + oc > 1)
+            cost += join * (double)(sc + oc) * (double)(share ? rows : rest * PA_ROWS);
         if (best < 0.0 || cost < best) {
             best = cost;
             p.chunk = chunk;
@@ -226,9 +243,14 @@ constexpr PrefixPlan prefix_plan(int num_seqs, int total_q, int max_q, int max_c
         if (chunk == tile)
             break;
     }
-    p.alike = share ? 0 : prefix_len / p.chunk;
     p.slots = p.shared_chunks + p.own_chunks;
-    p.blocks = (int64_t)p.shared_tiles * p.shared_chunks + (int64_t)p.own_tiles * p.own_chunks;
+    if (p.slots == 1 || rest == 0) {
+        p.whole = p.own_tiles;
+        p.own_chunks = p.slots = 1;
+    }
+    p.alike = share || p.whole ? 0 : prefix_len / p.chunk;
+    p.part_rows = p.slots == 1 ? 0 : share ? rows : (int64_t)(p.own_tiles - p.whole) * PA_ROWS;
+    p.blocks = (int64_t)p.shared_tiles * p.shared_chunks + p.whole + (int64_t)(p.own_tiles - p.whole) * p.own_chunks;
     return p;
 }
 
@@ -236,26 +258,28 @@ constexpr PrefixPlan prefix_plan(int num_seqs, int total_q, int max_q, int max_c
 // and blocks of one XCD (blk % 8) have consecutive numbers: the keys come into one L2.
 struct PrefixBlock {
     bool shared;
-    int tile, chunk, slot;
+    int tile, chunk;
+    int slot;  // -1: the tile's keys are not split
 };
-constexpr int64_t prefix_xcd(int64_t blk, int64_t n)
+constexpr int prefix_xcd(int blk, int n)
 {
-    const int64_t x = blk % PA_XCD, per = n / PA_XCD, more = n % PA_XCD;
+    const int x = blk % PA_XCD, per = n / PA_XCD, more = n % PA_XCD;
     return x * per + (x < more ? x : more) + blk / PA_XCD;
 }
-constexpr PrefixBlock prefix_block(const PrefixPlan &p, int64_t blk)
+constexpr PrefixBlock prefix_block(const PrefixPlan &p, int blk)
 {
-    const int64_t together = (int64_t)p.shared_tiles * p.shared_chunks;
+    const int together = p.shared_tiles * p.shared_chunks;
     if (blk < together) {
-        const int64_t id = prefix_xcd(blk, together);
-        const int c = (int)(id / p.shared_tiles);
-        return {true, (int)(id % p.shared_tiles), c, c};
+        const int id = prefix_xcd(blk, together), c = id / p.shared_tiles;
+        return {true, id - c * p.shared_tiles, c, c};
     }
     blk -= together;
-    const int64_t alike = (int64_t)p.own_tiles * p.alike;
-    const int64_t id = blk < alike ? prefix_xcd(blk, alike) : blk;
-    const int c = (int)(id / p.own_tiles);
-    return {false, (int)(id % p.own_tiles), c, p.shared_chunks + c};
+    if (blk < p.whole)
+        return {false, blk, 0, -1};
+    blk -= p.whole;
+    const int tiles = p.own_tiles - p.whole, alike = tiles * p.alike;
+    const int id = blk < alike ? prefix_xcd(blk, alike) : blk, c = id / tiles;
+    return {false, p.whole + id - c * tiles, c, p.shared_chunks + c};
 }
 
 } // namespace janus

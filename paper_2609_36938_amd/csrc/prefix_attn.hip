@@ -41,45 +41,59 @@ struct PrefixArgs {
     void *out;
     int out_f32;
     float *lse;
-    float *part;  // null: one range a row, written to out
+    float *part;  // O of the ranges, then their maxima and sums
     PrefixPlan plan;
 };
 
-// The block's rows, keys and table.
+// Session of an own tile, and the tile's rows (row0 >= row1: none).
+JANUS_DEV int tile_rows(const PrefixArgs &g, int tile, int &row0, int &row1)
+{
+    int lo = 0, hi = g.num_seqs - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (prefix_tile_first(g.q_start[mid], g.heads, mid) <= tile)
+            lo = mid;
+        else
+            hi = mid - 1;
+    }
+    const int q0 = g.q_start[lo];
+    row0 = q0 * g.heads + (tile - prefix_tile_first(q0, g.heads, lo)) * PA_ROWS;
+    row1 = min(row0 + PA_ROWS, g.q_start[lo + 1] * g.heads);
+    return lo;
+}
+
+// The block's rows, keys and table, and where its results go: to row `part` of the
+// workspace on, or (part < 0) to out.
 struct PrefixRange {
-    int row0, row1, kbeg, kend, sess, slot;
+    int row0, row1, kbeg, kend, sess;
+    int64_t part;
     bool shared;
 };
-JANUS_DEV PrefixRange prefix_range(const PrefixArgs &g, int64_t blk)
+JANUS_DEV PrefixRange prefix_range(const PrefixArgs &g, int blk)
 {
     const PrefixBlock bk = prefix_block(g.plan, blk);
     PrefixRange r;
     r.shared = bk.shared;
-    r.slot = bk.slot;
     r.sess = 0;
     if (bk.shared) {
         r.row0 = bk.tile * PA_ROWS;
         r.row1 = min(r.row0 + PA_ROWS, g.q_start[g.num_seqs] * g.heads);
         r.kbeg = bk.chunk * g.plan.chunk;
         r.kend = min(r.kbeg + g.plan.chunk, g.plan.prefix);
+        r.part = bk.slot * g.plan.part_rows + r.row0;
         return r;
     }
-    int lo = 0, hi = g.num_seqs - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (prefix_tile_first(g.q_start[mid], g.heads, mid) <= bk.tile)
-            lo = mid;
-        else
-            hi = mid - 1;
-    }
-    const int q0 = g.q_start[lo], q1 = g.q_start[lo + 1];
-    r.sess = lo;
-    r.row0 = q0 * g.heads + (bk.tile - prefix_tile_first(q0, g.heads, lo)) * PA_ROWS;
-    r.row1 = min(r.row0 + PA_ROWS, q1 * g.heads);
+    r.sess = tile_rows(g, bk.tile, r.row0, r.row1);
     r.kbeg = g.plan.prefix + bk.chunk * g.plan.chunk;
-    r.kend = r.row0 < r.row1
-                 ? min(r.kbeg + g.plan.chunk, last_cand(g.hist_len[lo], (r.row1 - 1) / g.heads - q0, g.es) + 1)
-                 : r.kbeg;
+    r.kend = r.kbeg;
+    if (r.row0 < r.row1) {
+        r.kend = last_cand(g.hist_len[r.sess], (r.row1 - 1) / g.heads - g.q_start[r.sess], g.es) + 1;
+        if (bk.slot >= 0)
+            r.kend = min(r.kend, r.kbeg + g.plan.chunk);
+    }
+    r.part = bk.slot < 0           ? -1
+             : g.plan.prefix > 0 ? bk.slot * g.plan.part_rows + r.row0
+                                 : bk.slot * g.plan.part_rows + (int64_t)(bk.tile - g.plan.whole) * PA_ROWS;
     return r;
 }
 // First key that the row's token does not attend to.
@@ -354,10 +368,10 @@ __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
     const float l = lsum + __shfl_xor(lsum, 32);
     if (!live)
         return;
-    if (g.part) {
-        const int64_t at = (int64_t)r.slot * g.plan.rows + row;
+    if (r.part >= 0) {
+        const int64_t at = r.part + (row - r.row0);
         if (hf == 0)
-            *(float2 *)(g.part + (int64_t)g.plan.slots * g.plan.rows * 128 + 2 * at) = float2{m, l};
+            *(float2 *)(g.part + g.plan.slots * g.plan.part_rows * 128 + 2 * at) = float2{m, l};
         if (nt > 0) {
 #pragma unroll
             for (int d = 0; d < NB; ++d)
@@ -422,12 +436,12 @@ JANUS_DEV void plain_rows(const PrefixArgs &g, const PrefixRange &r, const int *
             }
         }
         const v4f a = {acc[0], acc[1], acc[2], acc[3]}, b = {acc[4], acc[5], acc[6], acc[7]};
-        if (g.part) {
-            const int64_t at = (int64_t)r.slot * g.plan.rows + row;
+        if (r.part >= 0) {
+            const int64_t at = r.part + (row - r.row0);
             *(v4f *)(g.part + at * 512 + 8 * lane) = a;
             *(v4f *)(g.part + at * 512 + 8 * lane + 4) = b;
             if (lane == 0)
-                *(float2 *)(g.part + (int64_t)g.plan.slots * g.plan.rows * 512 + 2 * at) = float2{m, l};
+                *(float2 *)(g.part + g.plan.slots * g.plan.part_rows * 512 + 2 * at) = float2{m, l};
         } else {
             const float inv = l != 0.f ? 1.f / l : 0.f;
             store_out4(g.out, g.out_f32, (int64_t)row * 512 + 8 * lane, a * inv);
@@ -787,10 +801,10 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
         if (to >= r.row1)
             continue;
         const float mm = sM[at], ll = sL[at];
-        if (g.part) {
-            const int64_t slot = (int64_t)r.slot * g.plan.rows + to;
+        if (r.part >= 0) {
+            const int64_t slot = r.part + at;
             if (hf == 0 && wave == 0)
-                *(float2 *)(g.part + (int64_t)g.plan.slots * g.plan.rows * 512 + 2 * slot) = float2{mm, ll};
+                *(float2 *)(g.part + g.plan.slots * g.plan.part_rows * 512 + 2 * slot) = float2{mm, ll};
             if (nt > 0) {
 #pragma unroll
                 for (int d = 0; d < 4; ++d)
@@ -818,23 +832,32 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
 // A range without keys (l = 0) wrote no O.  A worker is DV / 8 lanes of eight dims;
 // WPR workers share a row's ranges, so that few rows of many ranges are not a chain of loads.
 template <int DV, int WPR>
-__global__ __launch_bounds__(256) void prefix_combine(const float *__restrict__ part, int slots, int rows,
-                                                      const int32_t *__restrict__ q_start, int num_seqs, int heads,
-                                                      void *__restrict__ out, int out_f32, float *__restrict__ lse)
+__global__ __launch_bounds__(256) void prefix_combine(PrefixArgs g)
 {
     constexpr int LANES = DV / 8, WORKERS = 256 / LANES;
     static_assert(WORKERS % WPR == 0, "whole rows in a block");
     __shared__ v4f sO[WPR > 1 ? 2 * 256 : 1];
     __shared__ float sL[WPR > 1 ? WORKERS : 1];
     const int worker = threadIdx.x / LANES, in = threadIdx.x % LANES, w = worker % WPR;
-    const int row = blockIdx.x * (WORKERS / WPR) + worker / WPR;
-    const bool live = row < min(rows, q_start[num_seqs] * heads);
-    const float2 *ml = (const float2 *)(part + (int64_t)slots * rows * DV) + (live ? row : 0);
-    const float *po = part + (int64_t)(live ? row : 0) * DV + 8 * in;
-    const int64_t step = (int64_t)rows * DV;
+    const int slots = g.plan.slots;
+    const int64_t rows = g.plan.part_rows, at = (int64_t)blockIdx.x * (WORKERS / WPR) + worker / WPR;
+    // the row of out that row `at` of the workspace is
+    int row = (int)min(at, rows - 1);
+    bool live = at < rows;
+    if (g.plan.prefix > 0) {
+        live = live && row < g.q_start[g.num_seqs] * g.heads;
+    } else {
+        int row0, row1;
+        tile_rows(g, g.plan.whole + row / PA_ROWS, row0, row1);
+        row = row0 + row % PA_ROWS;
+        live = live && row < row1;
+    }
+    const float2 *ml = (const float2 *)(g.part + slots * rows * DV) + (live ? at : 0);
+    const float *po = g.part + (live ? at : 0) * DV + 8 * in;
+    const int64_t step = rows * DV;
     float M = M_INIT;
     for (int s = in; s < slots; s += LANES) {
-        const float2 x = ml[(int64_t)s * rows];
+        const float2 x = ml[s * rows];
         M = x.y != 0.f ? fmaxf(M, x.x) : M;
     }
 #pragma unroll
@@ -848,7 +871,7 @@ __global__ __launch_bounds__(256) void prefix_combine(const float *__restrict__ 
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const int s = s0 + k * WPR;
-            x[k] = s < slots ? ml[(int64_t)s * rows] : float2{0.f, 0.f};
+            x[k] = s < slots ? ml[s * rows] : float2{0.f, 0.f};
         }
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -886,10 +909,10 @@ __global__ __launch_bounds__(256) void prefix_combine(const float *__restrict__ 
     if (!live)
         return;
     const float inv = L != 0.f ? 1.f / L : 0.f;
-    store_out4(out, out_f32, (int64_t)row * DV + 8 * in, a * inv);
-    store_out4(out, out_f32, (int64_t)row * DV + 8 * in + 4, b * inv);
-    if (lse && in == 0)
-        lse[row] = L != 0.f ? (M + log2f(L)) * LN2 : -INFINITY;
+    store_out4(g.out, g.out_f32, (int64_t)row * DV + 8 * in, a * inv);
+    store_out4(g.out, g.out_f32, (int64_t)row * DV + 8 * in + 4, b * inv);
+    if (g.lse && in == 0)
+        g.lse[row] = L != 0.f ? (M + log2f(L)) * LN2 : -INFINITY;
 }
 
 template <int DV>
@@ -899,8 +922,7 @@ static void launch_combine(const PrefixArgs &g, hipStream_t st)
     constexpr int WORKERS = 256 / (DV / 8);
     const bool one = g.plan.slots <= 4;
     const auto kernel = one ? &prefix_combine<DV, 1> : &prefix_combine<DV, WORKERS>;
-    hipLaunchKernelGGL(kernel, dim3(one ? ceil_div(g.plan.rows, WORKERS) : g.plan.rows), dim3(256), 0, st, g.part,
-                       g.plan.slots, g.plan.rows, g.q_start, g.num_seqs, g.heads, g.out, g.out_f32, g.lse);
+    hipLaunchKernelGGL(kernel, dim3(one ? ceil_div(g.plan.part_rows, WORKERS) : g.plan.part_rows), dim3(256), 0, st, g);
 }
 
 }  // namespace janus
@@ -922,11 +944,13 @@ extern "C" int janus_prefix_attn(const janus_batch *bt, const void *q, int Hq, i
     const bool mqa = dqk == 128 && dv == 128;
     if ((out_dt != JANUS_BF16 && out_dt != JANUS_F32) || (!mla && !mqa) || Hq > 128 || k_row_stride % 8 != 0 ||
         v_row_stride % 8 != 0 || k_row_stride > (1 << 24) || v_row_stride > (1 << 24) || !at(q, 16) ||
-        !at(k_pool, 16) || !at(v_pool, 16) || !at(out, 4) || (int64_t)bt->total_q * Hq >= (int64_t)1 << 31)
+        !at(k_pool, 16) || !at(v_pool, 16) || !at(out, 4) || (int64_t)bt->total_q * Hq + (int64_t)bt->num_seqs * PA_ROWS >= (int64_t)1 << 31)
         return JANUS_ERR_UNSUPPORTED;
-    const PrefixPlan plan = prefix_plan(bt->num_seqs, bt->total_q, bt->max_q, bt->max_ctx, bt->total_ctx, prefix_len,
-                                        Hq, mla);
-    const size_t need = plan.slots > 1 ? (size_t)plan.slots * plan.rows * (dv + 2) * sizeof(float) : 0;
+    const PrefixPlan plan =
+        prefix_plan(bt->num_seqs, bt->total_q, bt->max_ctx, bt->total_ctx, prefix_len, Hq, mla);
+    if (plan.blocks > PA_MAX_BLOCKS)
+        return JANUS_ERR_UNSUPPORTED;
+    const size_t need = plan.slots > 1 ? (size_t)plan.slots * plan.part_rows * (dv + 2) * sizeof(float) : 0;
     if (!workspace) {
         *workspace_bytes = need;
         return JANUS_OK;
@@ -955,14 +979,14 @@ extern "C" int janus_prefix_attn(const janus_batch *bt, const void *q, int Hq, i
     g.out = out;
     g.out_f32 = out_dt == JANUS_F32;
     g.lse = lse;
-    g.part = plan.slots > 1 ? (float *)workspace : nullptr;
+    g.part = (float *)workspace;
     g.plan = plan;
     hipStream_t st = as_stream(stream);
     if (mla)
         hipLaunchKernelGGL(page_size < 8 ? prefix_mla<true> : prefix_mla<false>, dim3(plan.blocks), dim3(PA_THREADS), 0, st, g);
     else
         hipLaunchKernelGGL(prefix_mqa, dim3(plan.blocks), dim3(PA_THREADS), 0, st, g);
-    if (!g.part)
+    if (plan.slots == 1)
         return launch_status();
     if (hipGetLastError() != hipSuccess)
         return JANUS_ERR_DEVICE;

@@ -52,8 +52,8 @@ def rotate(x, pos, inv_freq, off, layout, mag=1.0, inverse=False):
     return y, m
 
 
-def attention(q, k, v, hist, new, rows_of, scale, es=0):
-    """Dense causal attention.  rows_of(session, ids): pool rows.  Returns (out, lse, sum p |v|, and
+def attention(q, k, v, hist, new, rows_of, scale, es=0, tokens=None):
+    """Dense causal attention, of all tokens or those listed.  rows_of(session, ids): pool rows.  Returns (out, lse, sum p |v|, and
     the largest sum |q k| * |scale| of a row's logits)."""
     T, H, _ = q.shape
     dv = v.shape[1]
@@ -63,7 +63,7 @@ def attention(q, k, v, hist, new, rows_of, scale, es=0):
     for b, (M, N) in enumerate(zip(hist, new)):
         for i in range(N):
             n = (M + i + 1) >> es
-            if n > 0:
+            if n > 0 and (tokens is None or at in tokens):
                 r = rows_of(b, np.arange(n))
                 kk, vv = k[r], v[r]
                 x = q[at] @ kk.T * scale

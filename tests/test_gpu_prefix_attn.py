@@ -206,6 +206,17 @@ def test_long_contexts_in_ranges():
     c.check(*c.run())
 
 
+@pytest.mark.parametrize("kind,heads,hist,new,tokens", [
+    ("mla", 128, [1500, 1300], [150, 160], [0, 100, 149, 150, 255, 256, 257, 300, 309]),
+    ("mqa2", 16, [2000, 0], [3900, 601], [0, 7, 2000, 3899, 3900, 4095, 4096, 4097, 4103, 4104, 4400, 4500]),
+])
+def test_whole_rounds_and_a_split_rest(kind, heads, hist, new, tokens):
+    """More tiles than blocks run at a time: the first ones whole, the last ones in ranges."""
+    c = Case(hist, new, heads, kind, 0, 64)
+    print("prefix rest", kind, flush=True)
+    c.check(*c.run(), keep=np.array(tokens), tokens=set(tokens))
+
+
 def test_two_captured_calls_share_no_state():
     """Two calls captured into one graph with workspaces of their own, replayed; every replay equals the eager call."""
     a, b = Case([600, 620], [1, 1], 16, "mla", 600, 64), Case([900], [3], 8, "mqa2", 0, 64, seed=2)
