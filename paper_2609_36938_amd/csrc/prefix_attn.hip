@@ -829,19 +829,21 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
 
 // Joins the ranges of a row: with maxima m_s and sums l_s, M = max m_s and w_s =
 // 2^(m_s - M), O = sum w_s O_s / sum w_s l_s and lse = (M + log2 sum w_s l_s) ln 2.
-// A range without keys (l = 0) wrote no O.  A worker is DV / 8 lanes of eight dims;
-// WPR workers share a row's ranges, so that few rows of many ranges are not a chain of loads.
-template <int DV, int WPR>
+// A range without keys (l = 0) wrote no O.  A worker is LANES lanes of eight dims; WPR of them
+// share a piece of a row, so that few rows of many ranges are not a chain of loads.
+template <int DV, int LANES, int WPR>
 __global__ __launch_bounds__(256) void prefix_combine(PrefixArgs g)
 {
-    constexpr int LANES = DV / 8, WORKERS = 256 / LANES;
-    static_assert(WORKERS % WPR == 0, "whole rows in a block");
+    constexpr int PIECES = DV / (8 * LANES), WORKERS = 256 / LANES;
+    static_assert(WORKERS % WPR == 0, "whole pieces in a block");
     __shared__ v4f sO[WPR > 1 ? 2 * 256 : 1];
     __shared__ float sL[WPR > 1 ? WORKERS : 1];
     const int worker = threadIdx.x / LANES, in = threadIdx.x % LANES, w = worker % WPR;
     const int slots = g.plan.slots;
-    const int64_t rows = g.plan.part_rows, at = (int64_t)blockIdx.x * (WORKERS / WPR) + worker / WPR;
-    // the row of out that row `at` of the workspace is
+    const int64_t rows = g.plan.part_rows, id = (int64_t)blockIdx.x * (WORKERS / WPR) + worker / WPR;
+    const int64_t at = id / PIECES;  // row of the workspace
+    const int dim = 8 * (LANES * (int)(id % PIECES) + in);
+    // the row of out that it is
     int row = (int)min(at, rows - 1);
     bool live = at < rows;
     if (g.plan.prefix > 0) {
@@ -853,9 +855,10 @@ __global__ __launch_bounds__(256) void prefix_combine(PrefixArgs g)
         live = live && row < row1;
     }
     const float2 *ml = (const float2 *)(g.part + slots * rows * DV) + (live ? at : 0);
-    const float *po = g.part + (live ? at : 0) * DV + 8 * in;
+    const float *po = g.part + (live ? at : 0) * DV + dim;
     const int64_t step = rows * DV;
     float M = M_INIT;
+#pragma unroll 4
     for (int s = in; s < slots; s += LANES) {
         const float2 x = ml[s * rows];
         M = x.y != 0.f ? fmaxf(M, x.x) : M;
@@ -877,7 +880,7 @@ __global__ __launch_bounds__(256) void prefix_combine(PrefixArgs g)
         for (int k = 0; k < 4; ++k) {
             u[k] = v[k] = v4f{0.f, 0.f, 0.f, 0.f};
             if (x[k].y != 0.f) {
-                const v4f *src = (const v4f *)(po + (int64_t)(s0 + k * WPR) * step);
+                const v4f *src = (const v4f *)(po + (s0 + k * WPR) * step);
                 u[k] = src[0];
                 v[k] = src[1];
             }
@@ -909,20 +912,28 @@ __global__ __launch_bounds__(256) void prefix_combine(PrefixArgs g)
     if (!live)
         return;
     const float inv = L != 0.f ? 1.f / L : 0.f;
-    store_out4(g.out, g.out_f32, (int64_t)row * DV + 8 * in, a * inv);
-    store_out4(g.out, g.out_f32, (int64_t)row * DV + 8 * in + 4, b * inv);
-    if (g.lse && in == 0)
+    store_out4(g.out, g.out_f32, (int64_t)row * DV + dim, a * inv);
+    store_out4(g.out, g.out_f32, (int64_t)row * DV + dim + 4, b * inv);
+    if (g.lse && dim == 0)
         g.lse[row] = L != 0.f ? (M + log2f(L)) * LN2 : -INFINITY;
 }
 
 template <int DV>
 static void launch_combine(const PrefixArgs &g, hipStream_t st)
 {
-    // a worker a row up to four ranges: all of them are in flight at once
-    constexpr int WORKERS = 256 / (DV / 8);
-    const bool one = g.plan.slots <= 4;
-    const auto kernel = one ? &prefix_combine<DV, 1> : &prefix_combine<DV, WORKERS>;
-    hipLaunchKernelGGL(kernel, dim3(one ? ceil_div(g.plan.part_rows, WORKERS) : g.plan.part_rows), dim3(256), 0, st, g);
+    auto go = [&](auto lanes, auto wpr) {
+        constexpr int LANES = decltype(lanes)::value, WPR = decltype(wpr)::value;
+        hipLaunchKernelGGL((prefix_combine<DV, LANES, WPR>),
+                           dim3(ceil_div(g.plan.part_rows * (DV / (8 * LANES)) * WPR, 256 / LANES)), dim3(256), 0, st, g);
+    };
+    using std::integral_constant;
+    constexpr int ALL = DV / 8;  // lanes of a whole row
+    if (g.plan.slots <= 4)  // a worker has all of a row's ranges in flight at once
+        go(integral_constant<int, ALL>{}, integral_constant<int, 1>{});
+    else if (g.plan.part_rows * (DV / 128) <= (DV == 512 ? 512 : 4096))  // few rows: a block each, or to each quarter of one
+        go(integral_constant<int, 16>{}, integral_constant<int, 16>{});
+    else
+        go(integral_constant<int, ALL>{}, integral_constant<int, 4>{});
 }
 
 }  // namespace janus
