@@ -210,37 +210,44 @@ constexpr PrefixPlan prefix_plan(int num_seqs, int total_q, int max_ctx, int64_t
     p.whole = (int)(rounds * resident * p.own_tiles / apart);
     const int64_t rest = apart - rounds * resident, ids = p.own_tiles - p.whole;
     const int own = max_ctx - p.prefix;
-    const int64_t mean = total_ctx / num_seqs > p.prefix ? total_ctx / num_seqs - p.prefix : 0;
+    const int mean = total_ctx / num_seqs > p.prefix ? (int)(total_ctx / num_seqs) - p.prefix : 0;
     const int span = own > p.prefix ? own : p.prefix;
-    // Time of a split, in keys of a block: one round of blocks takes as long as its
-    // longest, more of them share the chip and leave a part of a block at the end.  Each
-    // block starts for `start` keys, and a range of a row costs `join` to write and read again.
-    // Fitted to 18 batches of 1 to 64 sessions, each with 28 chunk lengths (MLA: the chunk
-    // taken is 0.3% off the best one in the mean, MQA 3%; with time by whole
-    // rounds alone it was 6 and 13%).
-    const double start = 16, join = mla ? 0.006 : 0.02;
+    // Time of a split, in keys of a block.  Blocks that all run at once take as long as the
+    // longest; more of them share the chip and leave half a block at the end.  (Where
+    // tiles may be empty, MLA blocks run at once up to 94% of the chip: the places of
+    // empty ones are not all taken again.  Without them counted, up to 4/5.)  An MQA
+    // block beside another on its CU adds a third of its time.  Each block starts for 64 keys,
+    // and a range of a row costs a hundredth of a key to write and read again.  Fitted
+    // to 35 batches of 1 to 100 sessions, each with 27 chunk lengths: the chunk taken is
+    // 0.9% off the best one in the mean for MLA and 2.8% for MQA, 10% at most (whole
+    // rounds of blocks, a start of 128 or 256 keys and a join of 0.02 or 0.01: 6 and 13%
+    // in the mean of the first 18).
+    const double start = 64, join = 0.01, tail = 0.5, slack = 0.8, beside = mla ? 0.0 : 0.35;
+    const double room = (mla && heads % PA_ROWS != 0 ? 0.94 : 1.0) * resident;
     double best = -1.0;
     for (int n = 1; n <= 256; n += 1 + n / 16) {
         const int chunk = (span > n ? (span + n - 1) / n + tile - 1 : tile) / tile * tile;
         const int sc = share ? (prefix_len + chunk - 1) / chunk : 0, oc = own > 0 ? (own + chunk - 1) / chunk : 1;
-        const int64_t mine = mean > 0 ? (mean + chunk - 1) / chunk : 1;
-        const int64_t together = (int64_t)p.shared_tiles * sc, work = together + rest * mine;
+        const int mine = mean > 0 ? (mean + chunk - 1) / chunk : 1;
+        const double together = (double)p.shared_tiles * sc, work = together + (double)rest * mine;
         const double longest = chunk + start;
         double cost = longest;
-        if (together + ids * oc > resident && (double)work > (mla ? 0.85 : 1.0) * resident) {
-            const double all = (double)together * longest + (double)rest * ((double)mean + (double)mine * start);
-            const double shared_out = all / resident + 0.3 * longest;
-            cost = shared_out > longest ? shared_out : longest;
+        if (mla || work > PA_CUS)
+            cost *= 1.0 + beside;
+        if (together + (double)ids * oc > room && work > slack * resident) {
+            const double all = (double)p.shared_tiles * (p.prefix + sc * start) + (double)rest * (mean + mine * start);
+            const double spread = all * (1.0 + beside) / resident + tail * longest;
+            cost = spread > cost ? spread : cost;
         }
         if (sc + oc > 1)
-            cost += join * (double)(sc + oc) * (double)(share ? rows : rest * PA_ROWS);
+            cost += join * (sc + oc) * (double)(share ? rows : rest * PA_ROWS);
         if (best < 0.0 || cost < best) {
             best = cost;
             p.chunk = chunk;
             p.shared_chunks = sc;
             p.own_chunks = oc;
         }
-        if (chunk == tile)
+        if (chunk == tile || work > 8.0 * resident)
             break;
     }
     p.slots = p.shared_chunks + p.own_chunks;
