@@ -104,18 +104,69 @@ JANUS_DEV int row_limit(const PrefixArgs &g, const PrefixRange &r, int row)
     return min(r.kend, last_cand(g.hist_len[s], token - g.q_start[s], g.es) + 1);
 }
 
-// Parts of a bf16 pair word of V that are not finite: what is left, and the
-// largest finite value in the place of +inf or NaN (up), of -inf or NaN (down).
-JANUS_DEV void split_odd(int x, int &fin, int &up, int &down)
+// The block's rows without matrix instructions: a wave a row, a lane a key, then DV / 64 dims.
+// For blocks that hold an infinity or NaN in a row of V of a tile in which rows end
+// at different keys: a probability of 0 does not undo it for the rows without the key.
+template <int DQK, int DV>
+JANUS_DEV void plain_rows(const PrefixArgs &g, const PrefixRange &r, const int *lim)
 {
-    fin = up = down = 0;
+    constexpr int N = DV / 64;
+    const int lane = threadIdx.x & 63;
+    const int32_t *pt = g.table + (int64_t)r.sess * g.pt_ld;
+    auto slot = [&](int key) {
+        return ((int64_t)pt[key >> g.page_shift] << g.page_shift) + (key & ((1 << g.page_shift) - 1));
+    };
+    for (int row = r.row0 + (threadIdx.x >> 6); row < r.row1; row += PA_WAVES) {
+        const uint16_t *q = g.q + (int64_t)row * DQK;
+        const int end = lim[row - r.row0];
+        float m = M_INIT, l = 0.f, acc[N] = {};
+        for (int k0 = r.kbeg; k0 < end; k0 += 64) {
+            float x = -INFINITY;
+            if (k0 + lane < end) {
+                const uint16_t *k = (const uint16_t *)(g.k + slot(k0 + lane) * g.k_rb);
+                x = 0.f;
+                for (int e = 0; e < DQK; ++e)
+                    x = fmaf(bf16_to_f32(q[e]), bf16_to_f32(k[e]), x);
+                x *= g.scale_log2;
+            }
+            float top = x;
 #pragma unroll
-    for (int z = 0; z < 32; z += 16) {
-        const int v = x >> z & 0xffff;
-        const bool bad = (v & 0x7f80) == 0x7f80;
-        fin |= bad ? 0 : v << z;
-        up |= bad && v != 0xff80 ? 0x7f7f << z : 0;
-        down |= bad && v != 0x7f80 ? 0xff7f << z : 0;
+            for (int o = 1; o < 64; o <<= 1)
+                top = fmaxf(top, __shfl_xor(top, o));
+            const float mnew = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f(m - mnew);
+            m = mnew;
+            const float p = k0 + lane < end ? __builtin_amdgcn_exp2f(x - m) : 0.f;
+            l *= alpha;
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                acc[e] *= alpha;
+            for (int j = 0; j < min(64, end - k0); ++j) {
+                const float pj = __shfl(p, j);
+                const uint16_t *v = (const uint16_t *)(g.v + slot(k0 + j) * g.v_rb) + N * lane;
+                l += pj;
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    acc[e] = fmaf(pj, bf16_to_f32(v[e]), acc[e]);
+            }
+        }
+        const int64_t at = r.part + (row - r.row0);
+        const float inv = l != 0.f ? 1.f / l : 0.f;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const int64_t o = (int64_t)row * DV + N * lane + e;
+            if (r.part >= 0)
+                g.part[at * DV + N * lane + e] = acc[e];
+            else if (g.out_f32)
+                ((float *)g.out)[o] = acc[e] * inv;
+            else
+                ((__bf16 *)g.out)[o] = (__bf16)(acc[e] * inv);
+        }
+        if (lane == 0) {
+            if (r.part >= 0)
+                *(float2 *)(g.part + g.plan.slots * g.plan.part_rows * DV + 2 * at) = float2{m, l};
+            else if (g.lse)
+                g.lse[row] = l != 0.f ? (m + log2f(l)) * LN2 : -INFINITY;
+        }
     }
 }
 
@@ -135,6 +186,7 @@ __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
     constexpr int STEPS = 8, NB = 4, NK = PQ_KT / 32;    // K-steps, blocks of 32 dims and of 32 keys
     constexpr int GATHERS = KBUF / (1024 * PA_WAVES);    // a wave's, of each pool
     __shared__ __attribute__((aligned(16))) uint8_t ring[3 * BUF];
+    __shared__ int sLim[PA_ROWS];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c32 = lane & 31, hf = lane >> 5;
@@ -147,6 +199,8 @@ __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
     const int row = r.row0 + 32 * wave + c32;
     const bool live = row < r.row1;
     const int lim = row_limit(g, r, live ? row : r.row1 - 1);
+    if (hf == 0)
+        sLim[32 * wave + c32] = lim;
     int wmin = live ? lim : 0x7fffffff;  // keys before it are every row's of the wave
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1)
@@ -167,6 +221,7 @@ __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
         for (int i = 0; i < 16; ++i)
             o[d][i] = 0.f;
     float m = M_INIT, lsum = 0.f;
+    int bad = 0;  // a tile where rows end holds values of V that are not finite
 
     // Tiles begin at multiples of their length: a tile of longer pages lies in one.
     // A wave gathers four rows at a time, rows 16 j + 4 wave .. of K and of V.
@@ -198,6 +253,9 @@ __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
             }
         }
     };
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st)
+        asm volatile("" ::"v"(qf[st]));  // waited for here: a wait in the loop would be for the gathers too
     if (nt > 0) {
         issue(0, entry(0));
         issue(1, entry(1));
@@ -305,66 +363,33 @@ __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
         };
         // V^T P^T, its V operands read ahead likewise.
         constexpr int VALL = 2 * NK * NB, VAHEAD = 4;
-        // Where rows of the tile end at different keys, a probability of 0 does not undo an
-        // infinity or NaN that a row of V holds for another token.  With any of
-        // them in the tile, they are left out of the product, and come back as the
-        // overflow of products of large finite numbers, which are 0 for rows without the key.
-        bool odd = false;
-        if (!whole) {
-            int bad = 0;
-#pragma unroll 4
+        if (base < kbeg || base + PQ_KT > wmin) {
+#pragma unroll 1
             for (int w = 0; w < KBUF / 1024; ++w) {
                 const v4i x = *(const v4i *)(vt + 1024 * w + 16 * lane);
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     bad |= (x[e] & 0x7f80) == 0x7f80 || (x[e] & 0x7f800000) == 0x7f800000;
             }
-            odd = __ballot(bad) != 0;
         }
-        if (!odd) {
-            v8bf ahead[VAHEAD];
+        v8bf va[VAHEAD];
 #pragma unroll
-            for (int x = 0; x < VAHEAD; ++x)
-                ahead[x] = vop(x / NB, x % NB);
+        for (int x = 0; x < VAHEAD; ++x)
+            va[x] = vop(x / NB, x % NB);
 #pragma unroll
-            for (int x = 0; x < VALL; ++x) {
-                o[x % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ahead[x % VAHEAD], pb[x / NB], o[x % NB], 0, 0, 0);
-                if (x + VAHEAD < VALL)
-                    ahead[x % VAHEAD] = vop((x + VAHEAD) / NB, (x + VAHEAD) % NB);
-                __builtin_amdgcn_sched_barrier(0);
-            }
-        } else {
-#pragma unroll
-            for (int h = 0; h < 2 * NK; ++h) {
-                v4i has;  // the largest bf16 for keys that the row has
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const int key = base + 16 * h + 8 * (w / 2) + 4 * hf + 2 * (w % 2);
-                    has[w] = (key >= kbeg && key < lim ? 0x7f7f : 0) |
-                             (key + 1 >= kbeg && key + 1 < lim ? 0x7f7f0000 : 0);
-                }
-#pragma unroll
-                for (int d = 0; d < NB; ++d) {
-                    const v4i a = __builtin_bit_cast(v4i, vop(h, d));
-                    v4i fin, up, down;
-#pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        int x, y, z;
-                        split_odd(a[w], x, y, z);
-                        fin[w] = x;
-                        up[w] = y;
-                        down[w] = z;
-                    }
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_v8bf(fin), pb[h], o[d], 0, 0, 0);
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_v8bf(up), as_v8bf(has), o[d], 0, 0, 0);
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_v8bf(down), as_v8bf(has), o[d], 0, 0, 0);
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-            }
+        for (int x = 0; x < VALL; ++x) {
+            o[x % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[x % VAHEAD], pb[x / NB], o[x % NB], 0, 0, 0);
+            if (x + VAHEAD < VALL)
+                va[x % VAHEAD] = vop((x + VAHEAD) / NB, (x + VAHEAD) % NB);
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
 
     __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
+    if (__syncthreads_or(bad)) {
+        plain_rows<128, 128>(g, r, sLim);
+        return;
+    }
     const float l = lsum + __shfl_xor(lsum, 32);
     if (!live)
         return;
@@ -391,65 +416,6 @@ __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
                        v4f{o[d][i] * inv, o[d][i + 1] * inv, o[d][i + 2] * inv, o[d][i + 3] * inv});
     if (g.lse && hf == 0)
         g.lse[row] = l != 0.f ? (m + log2f(l)) * LN2 : -INFINITY;
-}
-
-// The block's rows without matrix instructions, a wave a row and a lane a key, then eight dims.
-JANUS_DEV void plain_rows(const PrefixArgs &g, const PrefixRange &r, const int *lim)
-{
-    const int lane = threadIdx.x & 63;
-    const int32_t *pt = g.table + (int64_t)r.sess * g.pt_ld;
-    auto key_row = [&](int key) {
-        return (const uint16_t *)(g.k + (((int64_t)pt[key >> g.page_shift] << g.page_shift) +
-                                         (key & ((1 << g.page_shift) - 1))) * g.k_rb);
-    };
-    for (int row = r.row0 + (threadIdx.x >> 6); row < r.row1; row += PA_WAVES) {
-        const uint16_t *q = g.q + (int64_t)row * 576;
-        const int end = lim[row - r.row0];
-        float m = M_INIT, l = 0.f, acc[8] = {};
-        for (int k0 = r.kbeg; k0 < end; k0 += 64) {
-            float x = -INFINITY;
-            if (k0 + lane < end) {
-                const uint16_t *k = key_row(k0 + lane);
-                x = 0.f;
-                for (int e = 0; e < 576; ++e)
-                    x = fmaf(bf16_to_f32(q[e]), bf16_to_f32(k[e]), x);
-                x *= g.scale_log2;
-            }
-            float top = x;
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1)
-                top = fmaxf(top, __shfl_xor(top, o));
-            const float mnew = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f(m - mnew);
-            m = mnew;
-            const float p = k0 + lane < end ? __builtin_amdgcn_exp2f(x - m) : 0.f;
-            l *= alpha;
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                acc[e] *= alpha;
-            for (int j = 0; j < min(64, end - k0); ++j) {
-                const float pj = __shfl(p, j);
-                const uint16_t *v = key_row(k0 + j) + 8 * lane;
-                l += pj;
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    acc[e] = fmaf(pj, bf16_to_f32(v[e]), acc[e]);
-            }
-        }
-        const v4f a = {acc[0], acc[1], acc[2], acc[3]}, b = {acc[4], acc[5], acc[6], acc[7]};
-        if (r.part >= 0) {
-            const int64_t at = r.part + (row - r.row0);
-            *(v4f *)(g.part + at * 512 + 8 * lane) = a;
-            *(v4f *)(g.part + at * 512 + 8 * lane + 4) = b;
-            if (lane == 0)
-                *(float2 *)(g.part + g.plan.slots * g.plan.part_rows * 512 + 2 * at) = float2{m, l};
-        } else {
-            const float inv = l != 0.f ? 1.f / l : 0.f;
-            store_out4(g.out, g.out_f32, (int64_t)row * 512 + 8 * lane, a * inv);
-            store_out4(g.out, g.out_f32, (int64_t)row * 512 + 8 * lane + 4, b * inv);
-            if (g.lse && lane == 0)
-                g.lse[row] = l != 0.f ? (m + log2f(l)) * LN2 : -INFINITY;
-        }
-    }
 }
 
 constexpr int PM_KT = 32, PM_STEPS = 576 / 16;
@@ -786,7 +752,7 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
     // Rows that end in a tile whose V holds an infinity or NaN: a probability of 0
     // does not undo it.  The block is done again, a row and a key at a time.
     if (__syncthreads_or(bad)) {
-        plain_rows(g, r, sLim);
+        plain_rows<576, 512>(g, r, sLim);
         return;
     }
     const float l = lsum + __shfl_xor(lsum, 32);

@@ -140,7 +140,6 @@ def test_what_is_masked_does_not_matter(kind, heads):
     """NaN and infinities in rows that a token does not attend to: later appended tokens' rows, rows of the pool that no
     session has, ids behind the last one, and table entries that are not used."""
     c = Case([290, 330], [20, 12], heads, kind, 200, 64)
-    clean = [t.clone() for t in c.run(out_dtype="f32")]
     used = np.zeros(len(c.k), bool)
     for b in range(2):
         used[c.rows_of(b, np.arange(c.hist[b] + c.new[b]))] = True
@@ -152,9 +151,6 @@ def test_what_is_masked_does_not_matter(kind, heads):
         pool[late] = bad[torch.from_numpy(np.arange(10) % 3)][:, None]
     got = c.run(out_dtype="f32")
     early = np.r_[0:10, 20:32]
-    if kind == "mqa2":                             # MLA blocks with such values take another order of sums
-        for g, w in zip(got, clean):
-            assert torch.equal(g[early], w[early])
     c.check(*got, keep=early)
     assert not torch.isfinite(got[0][10:20]).any()
 
@@ -163,19 +159,20 @@ def test_what_is_masked_does_not_matter(kind, heads):
 def test_an_infinity_goes_where_it_is_attended_to(kind):
     """Single values of V: +inf, -inf and NaN in dims of their own, in a row that the later tokens read."""
     c = Case([64], [40], 4, kind, 0, 64)
-    clean = c.run(out_dtype="f32")[0].clone()
     row = int(c.rows_of(0, np.array([80]))[0])
     v = c.v
     if kind == "mla":                              # K and V are one row: a query of 0 there keeps the logits
         c.q[:, :, :3] = 0
-        clean = c.run(out_dtype="f32")[0].clone()
     v[row, :3] = torch.tensor([float("inf"), float("-inf"), float("nan")]).bfloat16()
     if kind == "mla":                              # 0 * inf is NaN in the logits of the tokens that read it
         got = c.run(out_dtype="f32")[0]
         assert torch.isfinite(got[:16]).all() and torch.isnan(got[16:]).all()
         return
-    got = c.run(out_dtype="f32")[0]
-    assert torch.equal(got[:16], clean[:16]) and torch.equal(got[16:, :, 3:], clean[16:, :, 3:])
+    got, lse = c.run(out_dtype="f32")
+    v[row, :3] = 0                                 # the other dims, and the tokens before, are as without them
+    mask = got.clone()
+    mask[16:, :, :3] = c.run(out_dtype="f32")[0][16:, :, :3]
+    c.check(mask, lse)
     assert (got[16:, :, 0] == float("inf")).all() and (got[16:, :, 1] == float("-inf")).all()
     assert torch.isnan(got[16:, :, 2]).all()
 
