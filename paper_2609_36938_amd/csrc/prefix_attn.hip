@@ -45,16 +45,22 @@ struct PrefixArgs {
     PrefixPlan plan;
 };
 
-// Session of an own tile, and the tile's rows (row0 >= row1: none).
+// Session of an own tile, and the tile's rows (row0 >= row1: none).  WAVE: every lane of
+// the wave asks for the same tile, 64 sessions are looked at in one load.
+template <bool WAVE>
 JANUS_DEV int tile_rows(const PrefixArgs &g, int tile, int &row0, int &row1)
 {
-    int lo = 0, hi = g.num_seqs - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (prefix_tile_first(g.q_start[mid], g.heads, mid) <= tile)
-            lo = mid;
-        else
-            hi = mid - 1;
+    int lo = 0, hi = g.num_seqs;  // the session is in [lo, hi)
+    while (hi - lo > 1) {
+        if constexpr (WAVE) {
+            const int step = (hi - lo + kWave - 1) / kWave, s = lo + (int)(threadIdx.x & 63) * step;
+            const uint64_t below = __ballot(s < hi && prefix_tile_first(g.q_start[s], g.heads, s) <= tile);
+            lo += max((int)__popcll(below) - 1, 0) * step;
+            hi = min(hi, lo + step);
+        } else {
+            const int mid = (lo + hi) >> 1;
+            (prefix_tile_first(g.q_start[mid], g.heads, mid) <= tile ? lo : hi) = mid;
+        }
     }
     const int q0 = g.q_start[lo];
     row0 = q0 * g.heads + (tile - prefix_tile_first(q0, g.heads, lo)) * PA_ROWS;
@@ -83,7 +89,7 @@ JANUS_DEV PrefixRange prefix_range(const PrefixArgs &g, int blk)
         r.part = bk.slot * g.plan.part_rows + r.row0;
         return r;
     }
-    r.sess = tile_rows(g, bk.tile, r.row0, r.row1);
+    r.sess = tile_rows<true>(g, bk.tile, r.row0, r.row1);
     r.kbeg = g.plan.prefix + bk.chunk * g.plan.chunk;
     r.kend = r.kbeg;
     if (r.row0 < r.row1) {
@@ -100,6 +106,15 @@ JANUS_DEV PrefixRange prefix_range(const PrefixArgs &g, int blk)
 JANUS_DEV int row_limit(const PrefixArgs &g, const PrefixRange &r, int row)
 {
     const int token = row / g.heads;
+    if (r.shared && g.num_seqs <= 4 * kWave) {
+        // mostly all sessions reach behind the prefix: one load, where the search for each
+        // row's own is a chain of them
+        bool all = true;
+        for (int s = threadIdx.x & 63; s < g.num_seqs; s += kWave)
+            all = all && last_cand(g.hist_len[s], 0, g.es) + 1 >= r.kend;
+        if (__ballot(!all) == 0)
+            return r.kend;
+    }
     const int s = r.shared ? session_of_row(g.q_start, g.num_seqs, token) : r.sess;
     return min(r.kend, last_cand(g.hist_len[s], token - g.q_start[s], g.es) + 1);
 }
@@ -183,9 +198,9 @@ __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
 {
     constexpr int RB = 256;                              // bytes of a row
     constexpr int KBUF = PQ_KT * RB, BUF = 2 * KBUF;     // K rows, then V rows
-    constexpr int STEPS = 8, NB = 4, NK = PQ_KT / 32;    // K-steps, blocks of 32 dims and of 32 keys
+    constexpr int STEPS = 8, NB = 4;                     // K-steps, blocks of 32 dims
     constexpr int GATHERS = KBUF / (1024 * PA_WAVES);    // a wave's, of each pool
-    __shared__ __attribute__((aligned(16))) uint8_t ring[3 * BUF];
+    __shared__ __attribute__((aligned(16))) uint8_t ring[4 * BUF];
     __shared__ int sLim[PA_ROWS];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -233,7 +248,7 @@ __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
     const uint32_t koff = gr * (uint32_t)g.k_rb + gc, voff = gr * (uint32_t)g.v_rb + gc;
     auto entry = [&](int t) { return pt[min(base0 + t * PQ_KT, kend - 1) >> g.page_shift]; };
     auto issue = [&](int t, int page) {
-        uint8_t *dst = ring + t % 3 * BUF + 1024 * wave;
+        uint8_t *dst = ring + (t & 3) * BUF + 1024 * wave;
         const int base = base0 + t * PQ_KT;
         if (ps >= PQ_KT - 1 && base >= kbeg && base + PQ_KT <= kend) {
             const int64_t slot = ((int64_t)page << g.page_shift) + (base & ps) + 4 * wave;
@@ -259,72 +274,68 @@ __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
     if (nt > 0) {
         issue(0, entry(0));
         issue(1, entry(1));
+        issue(2, entry(2));
     }
-    int page = nt > 0 ? entry(2) : 0;
+    int page = nt > 0 ? entry(3) : 0;
 
-    const int kcol = (hf ^ swz16(c32)) * 16;  // K: chunk 2 st + hf of key c32
-    // V: this lane addresses key 16 s + 8 u + 4 hf + (lane / 4) % 4 and dims 32 d + 16 (lane / 16 % 2) + 4 (lane % 4)
-    const int vkey = 4 * hf + ((lane >> 2) & 3);
-    const int vch = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-    for (int t = 0; t < nt; ++t) {
-        // tile t has landed, the next one's gathers may be on their way (behind the last
+    // LDS offsets in a tile.  K: chunk 2 st + hf of key c32.  V: keys 8 u + 4 hf + (lane / 4) % 4
+    // (and 16 more) and dims 32 d + 16 (lane / 16 % 2) + 4 (lane % 4)
+    int kat[STEPS], vat[NB][2];
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st)
+        kat[st] = c32 * RB + 16 * ((2 * st + hf) ^ swz16(c32));
+#pragma unroll
+    for (int d = 0; d < NB; ++d)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int k = 8 * u + 4 * hf + ((lane >> 2) & 3);
+            vat[d][u] = k * RB + 16 * ((4 * d + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ swz16(k)) + 8 * (lane & 1);
+        }
+    auto logits = [&](const uint8_t *tile) {
+        v16f x;
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            x[i] = 0.f;
+#pragma unroll
+        for (int st = 0; st < STEPS; ++st)
+            x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_v8bf(*(const v4i *)(tile + kat[st])), qf[st], x, 0, 0, 0);
+        return x;
+    };
+    // A turn scores tile t + 1 while it takes the exponentials of tile t, then multiplies
+    // them with tile t's V.  (Behind the last tile it scores what the ring holds, for nothing.)
+    auto turn = [&](auto slot, int t, v16f &s, v16f &ahead) {
+        constexpr int SLOT = decltype(slot)::value;
+        // tile t + 1 has landed, the next one's gathers may be on their way (behind the last
         // tile they read its last key again)
         __builtin_amdgcn_s_waitcnt(vmcnt_only(2 * GATHERS));
         lds_barrier();
-        const int next = entry(t + 3);
-        issue(t + 2, page);
+        const int next = entry(t + 4);
+        issue(t + 3, page);
         page = next;
-        const uint8_t *tile = ring + t % 3 * BUF, *vt = tile + KBUF;
+        const uint8_t *vt = ring + SLOT * BUF + KBUF;
         const int base = base0 + t * PQ_KT;
-
-        // K operands are read AHEAD steps before their MFMA, with a scheduling
-        // fence a step: the compiler alone hoists as many reads as it finds, and spills.
-        v16f s[NK];
-        {
-            constexpr int AHEAD = 4, ALL = NK * STEPS;
-            auto kop = [&](int x) {
-                // step x / NK of keys 32 (x % NK) + c32
-                return *(const v4i *)(tile + (32 * (x % NK) + c32) * RB + (kcol ^ (32 * (x / NK))));
-            };
-            v4i ahead[AHEAD];
+        float mult = g.scale_log2;
+        if (base < kbeg || base + PQ_KT > wmin || mult <= 0.f) {
+            // keys 8 (i / 4) + 4 hf + i % 4 of this lane's row
 #pragma unroll
-            for (int x = 0; x < AHEAD; ++x)
-                ahead[x] = kop(x);
+            for (int i = 0; i < 16; ++i) {
+                const int key = base + 8 * (i / 4) + 4 * hf + i % 4;
+                s[i] = key >= kbeg && key < lim ? s[i] * mult : -INFINITY;
+            }
+            mult = 1.f;
+#pragma unroll 1
+            for (int w = 0; w < KBUF / 1024; ++w) {
+                const v4i x = *(const v4i *)(vt + 1024 * w + 16 * lane);
 #pragma unroll
-            for (int kb = 0; kb < NK; ++kb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    s[kb][i] = 0.f;
-#pragma unroll
-            for (int x = 0; x < ALL; ++x) {
-                const v4i a = ahead[x % AHEAD];
-                s[x % NK] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_v8bf(a), qf[x / NK], s[x % NK], 0, 0, 0);
-                if (x + AHEAD < ALL)
-                    ahead[x % AHEAD] = kop(x + AHEAD);
-                __builtin_amdgcn_sched_barrier(0);
+                for (int e = 0; e < 4; ++e)
+                    bad |= (x[e] & 0x7f80) == 0x7f80 || (x[e] & 0x7f800000) == 0x7f800000;
             }
         }
-        // keys 32 kb + 8 (i / 4) + 4 hf + i % 4 of this lane's row
-        const bool whole = base >= kbeg && base + PQ_KT <= wmin && g.scale_log2 > 0.f;
-        float mx = -INFINITY, mult = g.scale_log2;
-        if (whole) {
+        float mx = s[0];
 #pragma unroll
-            for (int kb = 0; kb < NK; ++kb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    mx = fmaxf(mx, s[kb][i]);
-            mx *= mult;
-        } else {
-#pragma unroll
-            for (int kb = 0; kb < NK; ++kb)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int key = base + 32 * kb + 8 * (i / 4) + 4 * hf + i % 4;
-                    s[kb][i] = key >= kbeg && key < lim ? s[kb][i] * mult : -INFINITY;
-                    mx = fmaxf(mx, s[kb][i]);
-                }
-            mult = 1.f;
-        }
+        for (int i = 1; i < 16; ++i)
+            mx = fmaxf(mx, s[i]);
+        mx *= mult;
         if (__ballot(mx > m + RESCALE_SLACK) != 0) {
             mx = fmaxf(mx, __shfl_xor(mx, 32));
             const float mnew = mx > m + RESCALE_SLACK ? mx : m;
@@ -337,51 +348,63 @@ __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
                 for (int i = 0; i < 16; ++i)
                     o[d][i] *= alpha;
         }
-        v8bf pb[2 * NK];
+        ahead = logits(ring + (SLOT + 1) % 4 * BUF);
+        v8bf pb[2];
 #pragma unroll
-        for (int kb = 0; kb < NK; ++kb)
+        for (int h = 0; h < 2; ++h) {
+            v8f p;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                v8f p;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    p[e] = __builtin_amdgcn_exp2f(s[kb][8 * h + e] * mult - m);
-                    lsum += p[e];
-                }
-                pb[2 * kb + h] = __builtin_convertvector(p, v8bf);
+            for (int e = 0; e < 8; ++e) {
+                p[e] = __builtin_amdgcn_exp2f(s[8 * h + e] * mult - m);
+                lsum += p[e];
             }
-        auto vop = [&](int h, int d) {
-            v8bf a;
-            v4s16 part[2];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const int k = 16 * h + 8 * u + vkey;
-                part[u] = lds_read_tr16(vt, k * RB + 16 * ((4 * d + vch) ^ swz16(8 * u + vkey)) + 8 * (lane & 1));
-            }
-            __builtin_memcpy(&a, part, 16);
-            return a;
-        };
-        // V^T P^T, its V operands read ahead likewise.
-        constexpr int VALL = 2 * NK * NB, VAHEAD = 4;
-        if (base < kbeg || base + PQ_KT > wmin) {
-#pragma unroll 1
-            for (int w = 0; w < KBUF / 1024; ++w) {
-                const v4i x = *(const v4i *)(vt + 1024 * w + 16 * lane);
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    bad |= (x[e] & 0x7f80) == 0x7f80 || (x[e] & 0x7f800000) == 0x7f800000;
-            }
+            pb[h] = __builtin_convertvector(p, v8bf);
         }
-        v8bf va[VAHEAD];
 #pragma unroll
-        for (int x = 0; x < VAHEAD; ++x)
-            va[x] = vop(x / NB, x % NB);
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int x = 0; x < VALL; ++x) {
-            o[x % NB] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[x % VAHEAD], pb[x / NB], o[x % NB], 0, 0, 0);
-            if (x + VAHEAD < VALL)
-                va[x % VAHEAD] = vop((x + VAHEAD) / NB, (x + VAHEAD) % NB);
-            __builtin_amdgcn_sched_barrier(0);
+            for (int d = 0; d < NB; ++d) {
+                v4s16 part[2];
+                v8bf a;
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+                    part[u] = lds_read_tr16(vt, vat[d][u] + 16 * RB * h);
+                __builtin_memcpy(&a, part, 16);
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, pb[h], o[d], 0, 0, 0);
+            }
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+        for (int x = 0; x < STEPS; ++x) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // a matrix instruction
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);  // an operand read
+            __builtin_amdgcn_sched_group_barrier(0x002, 7, 0);  // under it, seven others
+        }
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+        for (int x = 0; x < 2 * NB; ++x) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+        }
+    };
+    if (nt > 0) {
+        using std::integral_constant;
+        __builtin_amdgcn_s_waitcnt(vmcnt_only(4 * GATHERS));
+        lds_barrier();
+        v16f sa = logits(ring), sb;
+#pragma unroll 1
+        for (int t = 0;; t += 4) {
+            turn(integral_constant<int, 0>{}, t, sa, sb);
+            if (t + 1 >= nt)
+                break;
+            turn(integral_constant<int, 1>{}, t + 1, sb, sa);
+            if (t + 2 >= nt)
+                break;
+            turn(integral_constant<int, 2>{}, t + 2, sa, sb);
+            if (t + 3 >= nt)
+                break;
+            turn(integral_constant<int, 3>{}, t + 3, sb, sa);
+            if (t + 4 >= nt)
+                break;
         }
     }
 
@@ -816,7 +839,7 @@ __global__ __launch_bounds__(256) void prefix_combine(PrefixArgs g)
         live = live && row < g.q_start[g.num_seqs] * g.heads;
     } else {
         int row0, row1;
-        tile_rows(g, g.plan.whole + row / PA_ROWS, row0, row1);
+        tile_rows<false>(g, g.plan.whole + row / PA_ROWS, row0, row1);
         row = row0 + row % PA_ROWS;
         live = live && row < row1;
     }
