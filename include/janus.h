@@ -462,8 +462,8 @@ int janus_rotary_frequencies(int dim, double base, double factor, int scaling, i
  * attention; keys that stay out of a cache).
  *   x      device [total_q, heads, size], x_dt JANUS_F32 or JANUS_BF16; strides in
  *          elements between tokens and heads, a head's elements adjacent
- *   out    device, the same shape with its own strides, out_dt JANUS_F32,
- *          JANUS_BF16 or JANUS_FP8_E4M3.  It is x itself (same type and strides:
+ *   out    device, the same shape with its own strides, whose heads do not
+ *          overlap, out_dt JANUS_F32, JANUS_BF16 or JANUS_FP8_E4M3.  It is x itself (same type and strides:
  *          only the rotated elements are read and written) or shares no
  *          element with it.
  *   out_scale  device [total_q] fp32 for fp8, NULL otherwise

@@ -527,7 +527,7 @@ def rope(batch: Batch, rotary: Rotary, x, out=None, out_dtype: Optional[str] = N
     elif out_scale is not None:
         raise JanusError(f"{what}: out_scale goes with fp8 outputs")
     rotary._check(what, batch)
-    dev = _device(what, x, out, out_scale, batch.q_start, rotary.inv_freq)
+    dev = _device(what, x, out, out_scale, batch.q_start, rotary.inv_freq, rotary.positions)
     if batch.total_q:
         _launch(what, dev, stream, lib().janus_rope, batch.ref, rotary.ref, _at(x), xdt, x.stride(0), x.stride(1),
                 int(x.shape[1]), int(x.shape[2]), _at(out), odt, out.stride(0), out.stride(1), _at(out_scale))
@@ -570,7 +570,8 @@ def kv_append(batch: Batch, x, out, rotary: Optional[Rotary] = None, x_rot=None,
             raise JanusError(f"{what}: out_scale is to hold one float32 for each of {num_rows} rows")
     if rotary is not None:
         rotary._check(what, batch)
-    dev = _device(what, out, x, x_rot, rows, out_scale, batch.q_start, None if rotary is None else rotary.inv_freq)
+    dev = _device(what, out, x, x_rot, rows, out_scale, batch.q_start,
+                  *((rotary.inv_freq, rotary.positions) if rotary is not None else ()))
     if batch.total_q:
         _launch(what, dev, stream, lib().janus_kv_append, batch.ref, None if rotary is None else rotary.ref, _at(x),
                 xdt, 0 if x is None else x.stride(0), _at(x_rot), 0 if x_rot is None else x_rot.stride(0), n,

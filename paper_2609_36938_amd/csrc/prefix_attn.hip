@@ -808,9 +808,12 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
 #pragma unroll
         for (int d = 0; d < 4; ++d)
 #pragma unroll
-            for (int i = 0; i < 16; i += 4)
-                store_out4(g.out, g.out_f32, (int64_t)to * 512 + 128 * wave + 32 * d + 2 * i + 4 * hf,
-                           v4f{o[d][rb][i] * inv, o[d][rb][i + 1] * inv, o[d][rb][i + 2] * inv, o[d][rb][i + 3] * inv});
+            for (int i = 0; i < 16; i += 4) {
+                v4f x = {0.f, 0.f, 0.f, 0.f};
+                if (nt > 0)  // (without keys O has not been begun)
+                    x = v4f{o[d][rb][i] * inv, o[d][rb][i + 1] * inv, o[d][rb][i + 2] * inv, o[d][rb][i + 3] * inv};
+                store_out4(g.out, g.out_f32, (int64_t)to * 512 + 128 * wave + 32 * d + 2 * i + 4 * hf, x);
+            }
         if (g.lse && hf == 0 && wave == 0)
             g.lse[to] = ll != 0.f ? (mm + log2f(ll)) * LN2 : -INFINITY;
     }

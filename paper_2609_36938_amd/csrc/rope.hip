@@ -21,6 +21,7 @@
 
 #include <math.h>
 #include <type_traits>
+#include <utility>
 
 namespace janus {
 
@@ -383,6 +384,17 @@ static bool rotary_ok(const janus_rotary *r, int size)
            (r->layout == JANUS_ROTARY_HALVES || r->layout == JANUS_ROTARY_INTERLEAVED);
 }
 
+// Rows of `size` elements at these strides share none: the smaller stride holds a row,
+// the larger one all rows of the smaller.
+static bool apart(int64_t n1, int64_t s1, int64_t n2, int64_t s2, int64_t size)
+{
+    if (n1 <= 1 || (n2 > 1 && s2 < s1)) {
+        std::swap(n1, n2);
+        std::swap(s1, s2);
+    }
+    return n1 <= 1 || (s1 >= size && (n2 <= 1 || s2 >= s1 * (n1 - 1) + size));
+}
+
 static RopeArgs rope_args(const janus_batch *b, const janus_rotary *r)
 {
     RopeArgs g = {};
@@ -415,6 +427,8 @@ extern "C" int janus_rope(const janus_batch *b, const janus_rotary *r, const voi
 {
     if (!batch_ok(b) || !x || !out || heads < 1 || size < 1 || !rotary_ok(r, size) || !dtype_ok(x_dt) ||
         !dtype_ok(out_dt) || x_row_stride < 0 || x_head_stride < 0 || out_row_stride < 0 || out_head_stride < 0)
+        return JANUS_ERR_INVALID_ARG;
+    if (!apart(b->total_q, out_row_stride, heads, out_head_stride, size))
         return JANUS_ERR_INVALID_ARG;
     const bool fp8 = out_dt == JANUS_FP8_E4M3;
     if (fp8 != (out_scale != nullptr))

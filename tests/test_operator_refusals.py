@@ -60,10 +60,12 @@ def test_rope(L):
     assert call(st=(-1, 64)) == INVALID and call(ost=(128, -64)) == INVALID
     assert call(odt=2) == INVALID and call(odt=1, scale=FAKE) == INVALID    # a scale goes with fp8, and only with it
     assert call(xdt=7) == INVALID and call(odt=7) == INVALID
+    for ost in ((0, 64), (128, 0), (64, 64), (127, 64), (64, 200)):         # outputs on top of each other
+        assert call(ost=ost) == INVALID, ost
     assert call(xdt=2) == UNSUPPORTED
     assert call(out=FAKE, odt=0) == INVALID and call(out=FAKE, ost=(192, 64)) == INVALID  # in place: same type and strides
-    assert call(r=_rotary(2048), size=4096) == UNSUPPORTED
-    assert call(heads=1 << 12, size=1 << 13) == UNSUPPORTED
+    assert call(r=_rotary(2048), size=4096, ost=(8192, 4096)) == UNSUPPORTED
+    assert call(heads=1 << 12, size=1 << 13, ost=(1 << 25, 1 << 13)) == UNSUPPORTED
     assert call(b=_batch(total_q=0, max_ctx=0)) == OK                       # nothing to do
 
 
