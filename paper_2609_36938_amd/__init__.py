@@ -366,13 +366,12 @@ _SCALINGS = {None: 0, "linear": 1, "yarn": 2}
 
 def _device(what: str, *tensors) -> int:
     """Index of the one GPU that all the tensors (None: absent) are on."""
-    dev = -1
+    dev = tensors[0].get_device()  # -1 on the host
     for t in tensors:
-        if t is not None:
-            d = t.get_device()  # -1 on the host
-            if d < 0 or (d != dev and dev >= 0):
-                raise JanusError(f"{what}: tensors of one GPU expected")
-            dev = d
+        if t is not None and t.get_device() != dev:
+            dev = -1
+    if dev < 0:
+        raise JanusError(f"{what}: tensors of one GPU expected")
     return dev
 
 
@@ -394,7 +393,7 @@ def _launch(what: str, dev: int, stream, fn, *args):
     """fn(*args, stream) on GPU dev, whatever device is current.  (The raw stream: the object around it
     takes as long as the launch.)"""
     s = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
-    if torch.cuda.current_device() == dev:
+    if torch._C._cuda_getDevice() == dev:
         rc = fn(*args, s)
     else:
         with torch.cuda.device(dev):
@@ -467,22 +466,26 @@ def page_grow(batch: Batch, page_size: int, free_list, page_table, free_head=Non
     pages taken, the next free_head, pages short); out = (slots, counts) to
     write those tensors."""
     what = "janus_page_grow"
-    _want(what, "page_table", page_table, torch.int32, batch.c.num_seqs, None)
-    _want(what, "free_list", free_list, torch.int32, None)
+    i32, total, shape = torch.int32, batch.total_q, page_table.shape
+    if page_table.dtype is not i32 or len(shape) != 2 or shape[0] != batch.c.num_seqs or not page_table.is_contiguous():
+        _want(what, "page_table", page_table, i32, batch.c.num_seqs, None)
+    if free_list.dtype is not i32 or free_list.dim() != 1 or not free_list.is_contiguous():
+        _want(what, "free_list", free_list, i32, None)
+    if free_head is not None and (free_head.dtype is not i32 or free_head.numel() != 1):
+        raise JanusError(f"{what}: free_head is to be one int32")
     if out is None:
-        slots = torch.empty(batch.total_q, dtype=torch.int64, device=page_table.device)
-        counts = torch.empty(3, dtype=torch.int32, device=page_table.device)
+        slots = torch.empty(total, dtype=torch.int64, device=page_table.device)
+        counts = torch.empty(3, dtype=i32, device=page_table.device)
     else:
         slots, counts = out
-        _want(what, "slots", slots, torch.int64, batch.total_q)
-        _want(what, "counts", counts, torch.int32, 3)
+        _want(what, "slots", slots, torch.int64, total)
+        _want(what, "counts", counts, i32, 3)
     dev = _device(what, page_table, free_list, free_head, slots, counts, batch.q_start)
-    if free_head is not None and (free_head.dtype != torch.int32 or free_head.numel() != 1):
-        raise JanusError(f"{what}: free_head is to be one int32")
+    at = counts.data_ptr()
     # (an empty tensor has no address)
-    _launch(what, dev, stream, lib().janus_page_grow, batch.ref, int(page_size), _at(free_list),
-            int(free_list.numel()), _at(free_head), _at(page_table), _table(batch, page_table, page_size),
-            _at(slots) if batch.total_q else _at(counts), _at(counts))
+    _launch(what, dev, stream, lib().janus_page_grow, batch.ref, page_size, free_list.data_ptr(), free_list.numel(),
+            _at(free_head), page_table.data_ptr(), _table(batch, page_table, page_size),
+            slots.data_ptr() if total else at, at)
     return page_table, slots, counts
 
 
@@ -491,9 +494,12 @@ _ROPE_OUT = {"f32": (JANUS_F32, torch.float32), "bf16": (JANUS_BF16, torch.bfloa
 
 
 def _float_code(what: str, name: str, t) -> int:
-    if t.dtype not in (torch.float32, torch.bfloat16):
-        raise JanusError(f"{what}: {name} is to be float32 or bfloat16, not {t.dtype}")
-    return JANUS_F32 if t.dtype == torch.float32 else JANUS_BF16
+    dt = t.dtype
+    if dt is torch.bfloat16:
+        return JANUS_BF16
+    if dt is torch.float32:
+        return JANUS_F32
+    raise JanusError(f"{what}: {name} is to be float32 or bfloat16, not {dt}")
 
 
 def rope(batch: Batch, rotary: Rotary, x, out=None, out_dtype: Optional[str] = None, out_scale=None, stream=None):
@@ -505,37 +511,41 @@ def rope(batch: Batch, rotary: Rotary, x, out=None, out_dtype: Optional[str] = N
     one; out_dtype "f32", "bf16" or "fp8" (None: out's, or x's).  fp8 outputs are e4m3
     bytes (uint8, or float8_e4m3fn if given) with one scale per token."""
     what = "janus_rope"
-    if x.dim() != 3 or x.shape[0] != batch.total_q:
-        raise JanusError(f"{what}: x is to be [{batch.total_q}, heads, size], not {tuple(x.shape)}")
+    total, shape = batch.total_q, x.shape
+    if len(shape) != 3 or shape[0] != total:
+        raise JanusError(f"{what}: x is to be [{total}, heads, size], not {tuple(shape)}")
     xdt = _float_code(what, "x", x)
     if out_dtype is None:
-        out_dtype = "f32" if (x if out is None else out).dtype == torch.float32 else (
-            "bf16" if (x if out is None else out).dtype == torch.bfloat16 else "fp8")
+        given = (x if out is None else out).dtype
+        out_dtype = "bf16" if given is torch.bfloat16 else "f32" if given is torch.float32 else "fp8"
     if out_dtype not in _ROPE_OUT:
         raise JanusError(f"{what}: unknown out_dtype {out_dtype!r}")
     odt, torch_dt = _ROPE_OUT[out_dtype]
     if out is None:
-        out = torch.empty(tuple(x.shape), dtype=torch_dt, device=x.device)
-    if out.dtype != torch_dt and not (out_dtype == "fp8" and out.dtype == torch.float8_e4m3fn):
+        out = torch.empty(shape, dtype=torch_dt, device=x.device)
+    elif out.dtype is not torch_dt and not (out_dtype == "fp8" and out.dtype is torch.float8_e4m3fn):
         raise JanusError(f"{what}: out is {out.dtype}, not {out_dtype}")
-    if out.shape != x.shape or any(t.shape[2] > 1 and t.stride(2) != 1 for t in (x, out)):
+    xs, os_ = x.stride(), out.stride()
+    if out.shape != shape or (shape[2] > 1 and (xs[2] != 1 or os_[2] != 1)):
         raise JanusError(f"{what}: x and out are to have one shape and adjacent elements in a head")
     if out_dtype == "fp8":
         if out_scale is None:
-            out_scale = torch.empty(batch.total_q, dtype=torch.float32, device=x.device)
-        _want(what, "out_scale", out_scale, torch.float32, batch.total_q)
+            out_scale = torch.empty(total, dtype=torch.float32, device=x.device)
+        else:
+            _want(what, "out_scale", out_scale, torch.float32, total)
     elif out_scale is not None:
         raise JanusError(f"{what}: out_scale goes with fp8 outputs")
-    rotary._check(what, batch)
-    dev = _device(what, x, out, out_scale, batch.q_start, rotary.inv_freq, rotary.positions)
-    if batch.total_q:
-        _launch(what, dev, stream, lib().janus_rope, batch.ref, rotary.ref, _at(x), xdt, x.stride(0), x.stride(1),
-                int(x.shape[1]), int(x.shape[2]), _at(out), odt, out.stride(0), out.stride(1), _at(out_scale))
+    if rotary.positions is not None:
+        rotary._check(what, batch)
+    dev = _device(what, x, out, out_scale, batch.q_start, rotary.inv_freq)
+    if total:
+        _launch(what, dev, stream, lib().janus_rope, batch.ref, rotary.ref, x.data_ptr(), xdt, xs[0], xs[1], shape[1],
+                shape[2], out.data_ptr(), odt, os_[0], os_[1], _at(out_scale))
     return out, out_scale
 
 
 def kv_append(batch: Batch, x, out, rotary: Optional[Rotary] = None, x_rot=None, rows=None, out_scale=None,
-              size: Optional[int] = None, stream=None):
+              stream=None):
     """janus_kv_append: the appended tokens' rows into a cache; returns out.
 
     x [total_q, size] (float32 or bfloat16), or [total_q, size - rotary.dim] beside
@@ -545,37 +555,36 @@ def kv_append(batch: Batch, x, out, rotary: Optional[Rotary] = None, x_rot=None,
     bytes (uint8 or float8_e4m3fn) with their scales in out_scale (float32, one
     per row), or in the row behind its elements if that is None."""
     what = "janus_kv_append"
-    given = x if x is not None else x_rot
-    if given is None or any(t is not None and (t.dim() != 2 or t.shape[0] != batch.total_q or t.dtype != given.dtype or
-                                               (t.shape[1] > 1 and t.stride(1) != 1)) for t in (x, x_rot)):
-        raise JanusError(f"{what}: x and x_rot are to be [{batch.total_q}, elements] of one type, elements adjacent")
-    xdt = _float_code(what, "x", given)
-    n = sum(int(t.shape[1]) for t in (x, x_rot) if t is not None)
-    if size is not None and int(size) != n:
-        raise JanusError(f"{what}: the rows have {n} elements, not {size}")
-    if x_rot is not None and (rotary is None or x_rot.shape[1] != rotary.dim):
-        raise JanusError(f"{what}: x_rot holds the elements that rotary turns")
-    odt = _dtype_code(out, None)
-    if out.dim() < 1 or out.shape[-1] < n or not out.is_contiguous() or out.dtype == torch.int16:
+    total, n, given = batch.total_q, 0, x if x is not None else x_rot
+    for t in (x, x_rot):
+        if t is not None:
+            shape = t.shape
+            if len(shape) != 2 or shape[0] != total or t.dtype is not given.dtype or (shape[1] > 1 and t.stride(1) != 1):
+                raise JanusError(f"{what}: x and x_rot are to be [{total}, elements] of one type, elements adjacent")
+            n += shape[1]
+    if given is None or (x_rot is not None and (rotary is None or x_rot.shape[1] != rotary.dim)):
+        raise JanusError(f"{what}: x, or x_rot with the elements that rotary turns, or both")
+    xdt, odt = _float_code(what, "x", given), _dtype_code(out, None)
+    width = out.shape[-1] if out.dim() else 0
+    if width < n or not out.is_contiguous() or out.dtype is torch.int16:
         raise JanusError(f"{what}: out is to be contiguous rows of at least {n} elements, float32, bfloat16 or fp8")
-    num_rows = out.numel() // int(out.shape[-1])
+    num_rows = out.numel() // width
     if rows is not None:
-        _want(what, "rows", rows, torch.int64, batch.total_q)
+        _want(what, "rows", rows, torch.int64, total)
     elif num_rows < batch.total_ctx:
         raise JanusError(f"{what}: {num_rows} rows for {batch.total_ctx} keys")
     if out_scale is not None:
         if odt != JANUS_FP8_E4M3:
             raise JanusError(f"{what}: out_scale goes with fp8 rows")
-        if out_scale.dtype != torch.float32 or not out_scale.is_contiguous() or out_scale.numel() != num_rows:
+        if out_scale.dtype is not torch.float32 or not out_scale.is_contiguous() or out_scale.numel() != num_rows:
             raise JanusError(f"{what}: out_scale is to hold one float32 for each of {num_rows} rows")
-    if rotary is not None:
+    if rotary is not None and rotary.positions is not None:
         rotary._check(what, batch)
-    dev = _device(what, out, x, x_rot, rows, out_scale, batch.q_start,
-                  *((rotary.inv_freq, rotary.positions) if rotary is not None else ()))
-    if batch.total_q:
+    dev = _device(what, out, x, x_rot, rows, out_scale, batch.q_start, None if rotary is None else rotary.inv_freq)
+    if total:
         _launch(what, dev, stream, lib().janus_kv_append, batch.ref, None if rotary is None else rotary.ref, _at(x),
                 xdt, 0 if x is None else x.stride(0), _at(x_rot), 0 if x_rot is None else x_rot.stride(0), n,
-                _at(rows), num_rows, _at(out), odt, int(out.shape[-1]) * out.element_size(), _at(out_scale))
+                _at(rows), num_rows, out.data_ptr(), odt, width * out.element_size(), _at(out_scale))
     return out
 
 
