@@ -26,7 +26,6 @@
 namespace janus {
 
 constexpr int ROPE_THREADS = 256;
-constexpr int ROPE_UPT = 2;          // units in a lane's registers
 constexpr int ROPE_MAX_DIM = 1024;   // sines and cosines of a block fit in LDS
 constexpr float FP8_LARGEST = 448.f;
 constexpr float AMAX_FLOOR = 1e-12f;  // an all-zero row's scale stays positive
@@ -45,7 +44,7 @@ struct RopeArgs {
     uint8_t *out;
     int64_t o_rs, o_hs;          // bytes
     int plain_units;             // units a head of the elements that are only copied (0: in place)
-    int per_shift;               // log2 of a head's units, or -1
+    int turn_shift, plain_shift; // log2 of a head's units of both kinds, or -1
     int scatter;                 // cache rows: to `rows`, or by context where it is null
     const int64_t *rows;
     int64_t num_rows;
@@ -111,13 +110,12 @@ JANUS_DEV uint32_t bf16_pair(float a, float b)
 {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(v2f{a, b}, v2bf));
 }
-// To the nearest e4m3, ties to even; beyond the largest value: that value (NaN stays NaN).
+// To the nearest e4m3, ties to even (NaN stays NaN); the values are in its range.
 JANUS_DEV uint32_t fp8_quad(float a, float b, float c, float d)
 {
-    auto fit = [](float x) { return fabsf(x) > FP8_LARGEST ? copysignf(FP8_LARGEST, x) : x; };
     v2s w = {0, 0};
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, fit(a), fit(b), 1.0f, false);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, fit(c), fit(d), 1.0f, true);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, a, b, 1.0f, false);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(w, c, d, 1.0f, true);
     return __builtin_bit_cast(uint32_t, w);
 }
 
@@ -151,24 +149,32 @@ JANUS_DEV void store_group(uint8_t *p, const float (&v)[V], float inv)
 struct Unit {
     int head, a, b, pair;
 };
+// All heads' rotated units come first: a wave's lanes then mostly do the same.
 template <int V>
 JANUS_DEV Unit unit_at(const RopeArgs &g, int u)
 {
-    const int turned = g.dim / (2 * V), per = turned + g.plain_units;
+    auto over = [](int x, int n, int shift) { return shift >= 0 ? x >> shift : x / n; };
+    const int turned = g.dim / (2 * V), first = g.heads * turned;
     Unit at;
-    at.head = g.heads == 1 ? 0 : g.per_shift >= 0 ? u >> g.per_shift : u / per;
-    const int r = u - at.head * per;
-    const bool turns = r < turned;
-    const int e = 2 * V * (r - turned);  // among the plain elements
-    const int pa = e < g.off ? e : e + g.dim, pb = e + V < g.off ? e + V : e + V + g.dim;
-    const int ta = g.off + (g.halves ? r * V : 2 * r * V);
-    at.pair = turns ? r * V : -1;
-    at.a = turns ? ta : pa;
-    at.b = turns ? ta + (g.halves ? g.dim / 2 : V) : pb < g.size ? pb : -1;
+    if (u < first) {
+        at.head = g.heads == 1 ? 0 : over(u, turned, g.turn_shift);
+        at.pair = (u - at.head * turned) * V;
+        at.a = g.off + (g.halves ? at.pair : 2 * at.pair);
+        at.b = at.a + (g.halves ? g.dim / 2 : V);
+    } else {
+        u -= first;
+        at.head = g.heads == 1 ? 0 : over(u, g.plain_units, g.plain_shift);
+        const int e = 2 * V * (u - at.head * g.plain_units);  // among the plain elements
+        at.pair = -1;
+        at.a = e < g.off ? e : e + g.dim;
+        at.b = e + V < g.off ? e + V : e + V + g.dim;
+        if (at.b >= g.size)
+            at.b = -1;
+    }
     return at;
 }
 
-template <class T, int DT, int V, int LPR>
+template <class T, int DT, int V, int LPR, int UPT>
 __global__ __launch_bounds__(ROPE_THREADS) void rope_rows(RopeArgs g)
 {
     extern __shared__ float2 turn[];  // [rows of the block][dim / 2]: cosine, sine
@@ -180,19 +186,19 @@ __global__ __launch_bounds__(ROPE_THREADS) void rope_rows(RopeArgs g)
     const int row = live ? blockIdx.x * ROWS + mine : g.total_q - 1;
     const int pairs = g.dim / 2;
     const int units = g.heads * (g.dim / (2 * V) + g.plain_units);
-    // fp8 rows: all units of the token, LPR * ROPE_UPT at a time; others: the block's share of them
-    const int u0 = FP8 ? 0 : blockIdx.y * LPR * ROPE_UPT;
+    // fp8 rows: all units of the token, LPR * UPT at a time; others: the block's share of them
+    const int u0 = FP8 ? 0 : blockIdx.y * LPR * UPT;
 
     // Loads without a branch, so that all of them are under way at once: lanes
     // behind the last unit take it again, units of one group take that twice.
-    Unit at[ROPE_UPT];
-    Raw<T, V> ra[ROPE_UPT], rb[ROPE_UPT];
+    Unit at[UPT];
+    Raw<T, V> ra[UPT], rb[UPT];
     auto load = [&](int first) {
         const T *x = (const T *)g.x + (int64_t)row * g.x_rs;
         const T *xr = g.xr ? (const T *)g.xr + (int64_t)row * g.xr_rs - g.off : nullptr;
         const int skip = g.xr ? g.dim : 0;  // the rotated elements are elsewhere
 #pragma unroll
-        for (int k = 0; k < ROPE_UPT; ++k) {
+        for (int k = 0; k < UPT; ++k) {
             at[k] = unit_at<V>(g, min(first + k * LPR + lane, units - 1));
             const int a = at[k].a, b = at[k].b < 0 ? a : at[k].b;
             const bool other = at[k].pair >= 0 && g.xr;
@@ -234,10 +240,10 @@ __global__ __launch_bounds__(ROPE_THREADS) void rope_rows(RopeArgs g)
     else
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");  // (a token is one wave's or less)
 
-    float va[ROPE_UPT][V], vb[ROPE_UPT][V];
+    float va[UPT][V], vb[UPT][V];
     auto rotate = [&]() {
 #pragma unroll
-        for (int k = 0; k < ROPE_UPT; ++k) {
+        for (int k = 0; k < UPT; ++k) {
             ra[k].unpack(va[k]);
             rb[k].unpack(vb[k]);
             if (at[k].pair < 0)
@@ -266,7 +272,7 @@ __global__ __launch_bounds__(ROPE_THREADS) void rope_rows(RopeArgs g)
     constexpr int BYTES = FP8 ? 1 : DT == JANUS_BF16 ? 2 : 4;
     auto put = [&](int first, float inv) {
 #pragma unroll
-        for (int k = 0; k < ROPE_UPT; ++k) {
+        for (int k = 0; k < UPT; ++k) {
             if (first + k * LPR + lane >= units || !store)
                 continue;
             uint8_t *p = g.out + to * g.o_rs + (int64_t)at[k].head * g.o_hs;
@@ -279,40 +285,72 @@ __global__ __launch_bounds__(ROPE_THREADS) void rope_rows(RopeArgs g)
     if constexpr (!FP8) {
         put(u0, 1.f);
     } else {
-        // largest finite magnitude of the token
+        // Largest magnitude of the token (fmaxf passes over NaN), and if that is
+        // infinite, the largest finite one: infinities are then written as the largest e4m3.
+        const bool again = units > LPR * UPT;
         float top = 0.f;
+        bool finite = false;  // only finite ones
         auto tops = [&]() {
 #pragma unroll
-            for (int k = 0; k < ROPE_UPT; ++k)
+            for (int k = 0; k < UPT; ++k)
 #pragma unroll
                 for (int e = 0; e < V; ++e) {
                     const float a = fabsf(va[k][e]), b = fabsf(vb[k][e]);
-                    top = fmaxf(top, a < INFINITY ? a : 0.f);
-                    top = fmaxf(top, b < INFINITY ? b : 0.f);
+                    top = fmaxf(top, finite && !(a < INFINITY) ? 0.f : a);
+                    top = fmaxf(top, finite && !(b < INFINITY) ? 0.f : b);
                 }
         };
-        tops();
-        const bool again = units > LPR * ROPE_UPT;
-        for (int u = LPR * ROPE_UPT; u < units; u += LPR * ROPE_UPT) {
-            load(u);
-            rotate();
+        auto largest = [&]() {
+            top = 0.f;
             tops();
-        }
+            for (int u = LPR * UPT; u < units; u += LPR * UPT) {
+                load(u);
+                rotate();
+                tops();
+            }
 #pragma unroll
-        for (int o = 1; o < (LPR < kWave ? LPR : kWave); o <<= 1)
-            top = fmaxf(top, __shfl_xor(top, o));
-        if constexpr (LPR > kWave) {
-            if ((tid & 63) == 0)
-                red[tid >> 6] = top;
-            __syncthreads();
-            top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+            for (int o = 1; o < (LPR < kWave ? LPR : kWave); o <<= 1)
+                top = fmaxf(top, __shfl_xor(top, o));
+            if constexpr (LPR > kWave) {
+                if ((tid & 63) == 0)
+                    red[tid >> 6] = top;
+                __syncthreads();
+                top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+            }
+        };
+        auto fit = [&]() {
+#pragma unroll
+            for (int k = 0; k < UPT; ++k)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    va[k][e] = fabsf(va[k][e]) == INFINITY ? copysignf(top, va[k][e]) : va[k][e];
+                    vb[k][e] = fabsf(vb[k][e]) == INFINITY ? copysignf(top, vb[k][e]) : vb[k][e];
+                }
+        };
+        largest();
+        // (by blocks where a token is one: the second pass has a barrier)
+        const bool odd = LPR > kWave ? top == INFINITY : __ballot(top == INFINITY) != 0;
+        if (odd) {
+            if constexpr (LPR > kWave)
+                __syncthreads();
+            if (again) {
+                load(0);
+                rotate();
+            }
+            finite = true;
+            largest();
+            top = fmaxf(top, AMAX_FLOOR);
+            if (!again)
+                fit();
         }
         const float scale = fmaxf(top, AMAX_FLOOR) / FP8_LARGEST, inv = 1.f / scale;
         if (again) {
             // a row longer than the lanes' registers is read again
-            for (int u = 0; u < units; u += LPR * ROPE_UPT) {
+            for (int u = 0; u < units; u += LPR * UPT) {
                 load(u);
                 rotate();
+                if (odd)
+                    fit();
                 put(u, inv);
             }
         } else {
@@ -330,22 +368,30 @@ __global__ __launch_bounds__(ROPE_THREADS) void rope_rows(RopeArgs g)
 template <class T, int DT, int V>
 static void launch_rope_rows(RopeArgs g, hipStream_t st)
 {
-    const int per = g.dim / (2 * V) + g.plain_units, units = g.heads * per;
-    g.per_shift = pow2(per) ? __builtin_ctz((unsigned)per) : -1;
-    auto go = [&](auto lanes) {
-        constexpr int LPR = decltype(lanes)::value;
+    const int turned = g.dim / (2 * V), units = g.heads * (turned + g.plain_units);
+    g.turn_shift = pow2(turned) ? __builtin_ctz((unsigned)turned) : -1;
+    g.plain_shift = pow2(g.plain_units) ? __builtin_ctz((unsigned)g.plain_units) : -1;
+    auto go = [&](auto lanes, auto regs) {
+        constexpr int LPR = decltype(lanes)::value, UPT = decltype(regs)::value;
         const int rows = ROPE_THREADS / LPR;
-        hipLaunchKernelGGL((rope_rows<T, DT, V, LPR>),
-                           dim3(ceil_div(g.total_q, rows),
-                                DT == JANUS_FP8_E4M3 ? 1 : ceil_div(units, LPR * ROPE_UPT)),
+        hipLaunchKernelGGL((rope_rows<T, DT, V, LPR, UPT>),
+                           dim3(ceil_div(g.total_q, rows), DT == JANUS_FP8_E4M3 ? 1 : ceil_div(units, LPR * UPT)),
                            dim3(ROPE_THREADS), (size_t)rows * (g.dim / 2) * sizeof(float2), st, g);
     };
-    if (units <= 16 * ROPE_UPT)
-        go(std::integral_constant<int, 16>{});
-    else if (units <= 64 * ROPE_UPT)
-        go(std::integral_constant<int, 64>{});
+    // Many rows: the fewest lanes whose registers hold one, since a lane takes as many
+    // instructions whether or not it has a unit (8192 MLA rows, 36 units of 16 elements, 6.6 us
+    // on 16 lanes of three units, 7.4 on 64 lanes of two).  Few rows: one unit a lane (64 of them 4.6 us, 5.6).
+    using std::integral_constant;
+    if (V > 1 && units <= 16)
+        go(integral_constant<int, 16>{}, integral_constant<int, 1>{});
+    else if (units <= 48 && (V == 1 || g.total_q >= 4096))
+        go(integral_constant<int, 16>{}, integral_constant<int, 3>{});
+    else if (V > 1 && units <= 64)
+        go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+    else if (units <= 128)
+        go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
     else
-        go(std::integral_constant<int, 256>{});
+        go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
 }
 
 template <class T>

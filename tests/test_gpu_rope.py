@@ -128,16 +128,18 @@ def test_fp8_queries(heads, size, dim, off, dt):
     _close_fp8(_fp8(out).reshape(26, -1), scale, want.reshape(26, -1))
 
 
-def test_fp8_of_values_that_are_not_finite():
+@pytest.mark.parametrize("heads,size,dim", [(2, 32, 16), (64, 128, 64), (128, 576, 64), (3, 30, 10)])
+def test_fp8_of_values_that_are_not_finite(heads, size, dim):
     """An infinity becomes the largest value, NaN stays NaN, and neither moves the scale."""
-    x, xd = _inputs(3, 2, 32, "f32", 1)
-    x[1, 0, 20], x[1, 1, 21], x[1, 0, 22] = float("inf"), float("nan"), float("-inf")
-    xd[1, 0, [20, 22]] = xd[1, 1, 21] = 0
-    out, scale = janus.rope(janus.Batch([0], [3]), janus.Rotary(16), x, out_dtype="fp8")
+    x, xd = _inputs(3, heads, size, "f32", 1)
+    last = heads - 1
+    x[1, 0, size - 1], x[1, last, size - 2], x[1, 0, size - 3] = float("inf"), float("nan"), float("-inf")
+    xd[1, 0, [size - 1, size - 3]] = xd[1, last, size - 2] = 0
+    out, scale = janus.rope(janus.Batch([0], [3]), janus.Rotary(dim), x, out_dtype="fp8")
     got = _fp8(out)
-    assert got[1, 0, 20] == 448 and got[1, 0, 22] == -448 and np.isnan(got[1, 1, 21])
-    got[1, 0, [20, 22]] = got[1, 1, 21] = 0
-    _close_fp8(got.reshape(3, -1), scale, rotate(xd, np.arange(3), _freq(16)[0], 0, "half")[0].reshape(3, -1))
+    assert got[1, 0, size - 1] == 448 and got[1, 0, size - 3] == -448 and np.isnan(got[1, last, size - 2])
+    got[1, 0, [size - 1, size - 3]] = got[1, last, size - 2] = 0
+    _close_fp8(got.reshape(3, -1), scale, rotate(xd, np.arange(3), _freq(dim)[0], 0, "half")[0].reshape(3, -1))
 
 
 def test_rows_behind_the_last_session_stay():
@@ -222,6 +224,18 @@ def test_append_index_keys(es):
     _close_fp8(_fp8(keys)[at], scale[at], y[tokens])
     left = np.setdiff1d(np.arange(bt.total_ctx), at)
     assert (keys[left] == 9).all() and (scale[left] == -1).all()
+
+
+@pytest.mark.parametrize("rows", [4095, 4096, 5000])
+def test_many_rows(rows):
+    """Rows of the MLA cache on either side of the rule on lanes."""
+    x, xd = _inputs(rows, 1, 576, "bf16", 8)
+    pool = torch.zeros((rows, 592), dtype=torch.uint8, device="cuda")
+    janus.kv_append(janus.Batch([77], [rows]), x[:, 0], pool, janus.Rotary(64, 512),
+                    rows=torch.arange(rows, device="cuda").flip(0))
+    want = rotate(xd, positions([77], [rows]), _freq(64)[0], 512, "half")[0][:, 0]
+    got = pool.flip(0)
+    _close_fp8(_fp8(got[:, :576].contiguous()), got[:, 576:580].contiguous().view(torch.float32)[:, 0], want)
 
 
 def test_far_rows():
