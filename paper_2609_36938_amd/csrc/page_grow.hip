@@ -20,9 +20,10 @@ struct Growth {
 };
 JANUS_DEV Growth growth(int M, int N, int es, int page_shift)
 {
-    const int up = (1 << page_shift) - 1;
-    const int had = (entries_of(M, es) + up) >> page_shift;
-    return {had, ((entries_of(M + N, es) + up) >> page_shift) - had};
+    // (rounded up without a sum: entries and pages may be near 2^31)
+    auto pages = [&](int n) { return (n >> page_shift) + ((n & ((1 << page_shift) - 1)) != 0); };
+    const int had = pages(entries_of(M, es));
+    return {had, pages(entries_of(M + N, es)) - had};
 }
 
 // Sum over the block; every thread gets it.
@@ -45,14 +46,14 @@ __global__ __launch_bounds__(GROW_THREADS) void page_grow(
     __shared__ int red[GROW_THREADS / kWave];
     static_assert(GROW_THREADS == 4 * kWave, "block_sum adds four waves");
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int row = blockIdx.x * GROW_THREADS + tid;
-    const int r1 = min((int)(blockIdx.x + 1) * GROW_THREADS, total_q);
+    const int r0 = blockIdx.x * GROW_THREADS, r1 = r0 + min(GROW_THREADS, total_q - r0);
+    const bool live = tid < r1 - r0;
+    const int row = live ? r0 + tid : 0;
     const int head = free_head ? *free_head : 0;
     int next = head;  // free list entry of the first page of the sessions scanned next
     int s0 = 0;       // first of them
     if (num_seqs > GROW_THREADS && blockIdx.x > 0) {
         // sessions that end before this block's rows: how many, and their pages
-        const int r0 = blockIdx.x * GROW_THREADS;
         int before = 0, pages = 0;
         for (int s = tid; s < num_seqs; s += GROW_THREADS) {
             const int a = q_start[s], e = q_start[s + 1];
@@ -65,7 +66,7 @@ __global__ __launch_bounds__(GROW_THREADS) void page_grow(
         next += block_sum(pages, red);
     }
     int64_t slot = -1;
-    bool open = row < total_q;  // no session found yet
+    bool open = live;  // no session found yet
     for (; s0 < num_seqs; s0 += GROW_THREADS) {
         const int s = s0 + tid;
         int a = 0x7fffffff, e = 0x7fffffff, M = 0;
@@ -124,7 +125,7 @@ __global__ __launch_bounds__(GROW_THREADS) void page_grow(
         if (end >= r1)
             break;  // (uniform) the later sessions have no row here
     }
-    if (row < total_q)
+    if (live)
         slots[row] = slot;
     // the last block has seen every session that appends
     if (blockIdx.x == gridDim.x - 1 && tid == 0) {

@@ -75,6 +75,24 @@ def test_list_too_short(spare):
         assert np.array_equal(g.cpu().numpy(), w)
 
 
+@pytest.mark.parametrize("hist,new", [(0, 2**31 - 1), (2**31 - 300, 299)])
+def test_lengths_near_32_bits(hist, new):
+    """The last block's rows, and pages rounded up, end at 2^31."""
+    page, pages = 1 << 20, 1 << 11
+    had = -(-hist // page)
+    bt = janus.Batch([hist], [new])
+    table = torch.full((1, pages), -7, dtype=torch.int32, device="cuda")
+    table[0, :had] = torch.arange(had, dtype=torch.int32, device="cuda")
+    free = torch.arange(had, pages, dtype=torch.int32, device="cuda")
+    print("page_grow", hist, new, flush=True)
+    table, slots, counts = janus.page_grow(bt, page, free, table)
+    assert torch.equal(table[0], torch.arange(pages, dtype=torch.int32, device="cuda"))
+    assert counts.tolist() == [pages - had, pages - had, 0]
+    for a in range(0, new, 1 << 27):
+        part = slots[a:a + (1 << 27)]
+        assert torch.equal(part, torch.arange(hist + a, hist + a + part.numel(), device="cuda"))
+
+
 def test_no_tokens():
     hist, new, free, table = _case([10, 70], [0, 0], 64)
     got = _run(hist, new, 64, 0, free, 3, table)[3]
