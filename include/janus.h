@@ -472,7 +472,7 @@ int janus_rotary_frequencies(int dim, double base, double factor, int scaling, i
  * out = the nearest e4m3 of value / out_scale (infinities as the largest value, NaN as
  * NaN).  Angles are reduced in fp64, the rotation is fp32, and results are
  * rounded to out_dt once.  Rows from q_start[B] on are left as they are.
- * heads * size up to 2^24 (else JANUS_ERR_UNSUPPORTED).
+ * heads * size up to 2^24 and fewer than 2^24 tokens (else JANUS_ERR_UNSUPPORTED).
  */
 int janus_rope(const janus_batch *b, const janus_rotary *r, const void *x, janus_dtype x_dt,
                int64_t x_row_stride, int64_t x_head_stride, int heads, int size,
@@ -493,14 +493,15 @@ int janus_rope(const janus_batch *b, const janus_rotary *r, const void *x, janus
  *            No row twice.  NULL: row ctx_start[b] + c of the entry c that the
  *            token completes (the key arrays of janus_index_scores).
  *   out      device, num_rows rows of out_row_bytes bytes, whose first `size` elements
- *            are written; the other rows, and bytes behind a row, stay
+ *            are written; the other rows, and bytes behind a row, stay.  It
+ *            shares no element with x and x_rot.
  *   out_dt   JANUS_F32, JANUS_BF16 or JANUS_FP8_E4M3.  fp8 rows are quantised like
  *            janus_rope's; their scale goes to out_scale[row] (device
  *            [num_rows] fp32), or with out_scale == NULL to byte `size` of the
  *            row (janus_sparse_attn_fp8kv's rows: size 576, 592 bytes).
  * A scale in the row needs size and out_row_bytes in multiples of 4 and out
- * 4-byte aligned (else JANUS_ERR_UNSUPPORTED), as does size up to 2^24.  Rows from
- * q_start[B] on are skipped.
+ * 4-byte aligned; size is up to 2^24 and the tokens are fewer than 2^24 (else
+ * JANUS_ERR_UNSUPPORTED).  Rows from q_start[B] on are skipped.
  */
 int janus_kv_append(const janus_batch *b, const janus_rotary *r, const void *x, janus_dtype x_dt,
                     int64_t x_row_stride, const void *x_rot, int64_t x_rot_stride, int size,
@@ -524,12 +525,13 @@ int janus_kv_append(const janus_batch *b, const janus_rotary *r, const void *x, 
  *   q, pools, strides, page_table, softmax_scale, out, lse: as janus_sparse_attn
  *   workspace, workspace_bytes: as janus_sparse_attn_split
  * Shapes: MLA (dqk = 576, dv = 512, v_pool == k_pool, equal strides) and MQA
- * (dqk = dv = 128), each with 1 <= Hq <= 128, q and pools 16-byte aligned and
- * row strides in multiples of 8 up to 2^24, total_q * Hq + 128 B < 2^31 and
- * fewer than 2^24 blocks of 128 rows; else JANUS_ERR_UNSUPPORTED.  A workspace that is used must be 16-byte aligned, and out 4-byte aligned (else
- * JANUS_ERR_UNSUPPORTED).  A token with no candidate gets out = 0 and lse = -inf.  Rows from
- * q_start[B] on are left as they are.  Ids that a token does not attend to
- * do not touch its result, whatever their rows hold.
+ * (dqk = dv = 128), each with 1 <= Hq <= 128, q and pools 16-byte aligned, out
+ * 4-byte aligned, a workspace that is used 16-byte aligned, row strides in
+ * multiples of 8 up to 2^24, max_ctx up to 2^30, total_q * Hq + 128 B < 2^31 and
+ * fewer than 2^24 blocks of 128 rows; else JANUS_ERR_UNSUPPORTED.  A token with
+ * no candidate gets out = 0 and lse = -inf.  Rows from q_start[B] on are left as
+ * they are.  Ids that a token does not attend to do not touch its result,
+ * whatever their rows hold.
  */
 int janus_prefix_attn(const janus_batch *b, const void *q, int Hq, int dqk, int dv,
                       const void *k_pool, const void *v_pool,

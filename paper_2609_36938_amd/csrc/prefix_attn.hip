@@ -947,7 +947,8 @@ extern "C" int janus_prefix_attn(const janus_batch *bt, const void *q, int Hq, i
     const bool mqa = dqk == 128 && dv == 128;
     if ((out_dt != JANUS_BF16 && out_dt != JANUS_F32) || (!mla && !mqa) || Hq > 128 || k_row_stride % 8 != 0 ||
         v_row_stride % 8 != 0 || k_row_stride > (1 << 24) || v_row_stride > (1 << 24) || !at(q, 16) ||
-        !at(k_pool, 16) || !at(v_pool, 16) || !at(out, 4) || (int64_t)bt->total_q * Hq + (int64_t)bt->num_seqs * PA_ROWS >= (int64_t)1 << 31)
+        !at(k_pool, 16) || !at(v_pool, 16) || !at(out, 4) || bt->max_ctx > (1 << 30) ||
+        (int64_t)bt->total_q * Hq + (int64_t)bt->num_seqs * PA_ROWS >= (int64_t)1 << 31)
         return JANUS_ERR_UNSUPPORTED;
     const PrefixPlan plan =
         prefix_plan(bt->num_seqs, bt->total_q, bt->max_ctx, bt->total_ctx, prefix_len, Hq, mla);

@@ -27,6 +27,7 @@ namespace janus {
 
 constexpr int ROPE_THREADS = 256;
 constexpr int ROPE_MAX_DIM = 1024;   // sines and cosines of a block fit in LDS
+constexpr int ROPE_MAX_ROWS = 1 << 24;  // a launch takes fewer than 2^32 threads, 256 for the longest rows
 constexpr float FP8_LARGEST = 448.f;
 constexpr float AMAX_FLOOR = 1e-12f;  // an all-zero row's scale stays positive
 
@@ -482,7 +483,8 @@ extern "C" int janus_rope(const janus_batch *b, const janus_rotary *r, const voi
     const bool in_place = out == x;
     if (in_place && (x_dt != out_dt || x_row_stride != out_row_stride || x_head_stride != out_head_stride))
         return JANUS_ERR_INVALID_ARG;
-    if (x_dt == JANUS_FP8_E4M3 || r->dim > ROPE_MAX_DIM || (int64_t)heads * size > (1 << 24))
+    if (x_dt == JANUS_FP8_E4M3 || r->dim > ROPE_MAX_DIM || (int64_t)heads * size > (1 << 24) ||
+        b->total_q >= ROPE_MAX_ROWS)
         return JANUS_ERR_UNSUPPORTED;
     if (b->total_q == 0)
         return JANUS_OK;
@@ -514,7 +516,8 @@ extern "C" int janus_kv_append(const janus_batch *b, const janus_rotary *r, cons
     const bool fp8 = out_dt == JANUS_FP8_E4M3, inlined = fp8 && !out_scale;
     if (out_row_bytes < size * ob + (inlined ? 4 : 0) || out_row_bytes % ob != 0 || (out_scale && !fp8))
         return JANUS_ERR_INVALID_ARG;
-    if (x_dt == JANUS_FP8_E4M3 || (r && r->dim > ROPE_MAX_DIM) || size > (1 << 24))
+    if (x_dt == JANUS_FP8_E4M3 || (r && r->dim > ROPE_MAX_DIM) || size > (1 << 24) ||
+        b->total_q >= ROPE_MAX_ROWS)
         return JANUS_ERR_UNSUPPORTED;
     // the scale in the row is one aligned word
     if (inlined && (size % 4 != 0 || out_row_bytes % 4 != 0 || (reinterpret_cast<uintptr_t>(out) & 3) != 0))

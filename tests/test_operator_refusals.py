@@ -125,6 +125,19 @@ def test_prefix_attn(L):
     assert call(b=long, ld=2000, ws=ctypes.c_void_p(0x1008), size=ctypes.c_size_t(need.value)) == UNSUPPORTED
 
 
+def test_sizes_beyond_a_launch(L):
+    """Refused before anything is enqueued: 2^24 tokens of rows, keys beyond 2^30."""
+    many = _batch(total_q=1 << 24, max_ctx=1 << 24)
+    r, big = _rotary(), ctypes.c_size_t(1 << 62)
+    assert L.janus_rope(ctypes.byref(many), ctypes.byref(r), FAKE, 1, 64, 64, 1, 64, ctypes.c_void_p(0x9000), 1, 64, 64, None,
+                        None) == UNSUPPORTED
+    assert L.janus_kv_append(ctypes.byref(many), ctypes.byref(r), FAKE, 1, 64, None, 0, 64, FAKE, 100, FAKE, 1, 128, None,
+                             None) == UNSUPPORTED
+    far = _batch(total_q=1, max_ctx=(1 << 30) + 1)
+    assert L.janus_prefix_attn(ctypes.byref(far), FAKE, 8, 128, 128, FAKE, FAKE, 128, 128, FAKE, 1 << 15, 1 << 16, 0,
+                               ctypes.c_float(0.1), FAKE, 1, None, FAKE, ctypes.byref(big), None) == UNSUPPORTED
+
+
 def test_frequencies(L):
     freq, mag = janus.rotary_frequencies(64, 10000.0)
     assert mag == 1.0 and np.allclose(freq, 10000.0 ** (-np.arange(32) / 32), rtol=1e-14)
