@@ -389,10 +389,24 @@ def _at(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
+def _empty(shape, dtype, device, stream):
+    """A new tensor that belongs to the stream of the launch: its memory is not given to other
+    streams' work before, or after it is dropped, while that launch may use it."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _launch(what: str, dev: int, stream, fn, *args):
     """fn(*args, stream) on GPU dev, whatever device is current.  (The raw stream: the object around it
     takes as long as the launch.)"""
-    s = torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream
+    if stream is None:
+        s = torch._C._cuda_getCurrentRawStream(dev)
+    else:
+        s = stream.cuda_stream
+        if stream.device_index != dev:
+            raise JanusError(f"{what}: tensors of GPU {dev}, a stream of GPU {stream.device_index}")
     if torch._C._cuda_getDevice() == dev:
         rc = fn(*args, s)
     else:
@@ -474,8 +488,8 @@ def page_grow(batch: Batch, page_size: int, free_list, page_table, free_head=Non
     if free_head is not None and (free_head.dtype is not i32 or free_head.numel() != 1):
         raise JanusError(f"{what}: free_head is to be one int32")
     if out is None:
-        slots = torch.empty(total, dtype=torch.int64, device=page_table.device)
-        counts = torch.empty(3, dtype=i32, device=page_table.device)
+        slots = _empty(total, torch.int64, page_table.device, stream)
+        counts = _empty(3, i32, page_table.device, stream)
     else:
         slots, counts = out
         _want(what, "slots", slots, torch.int64, total)
@@ -522,7 +536,7 @@ def rope(batch: Batch, rotary: Rotary, x, out=None, out_dtype: Optional[str] = N
         raise JanusError(f"{what}: unknown out_dtype {out_dtype!r}")
     odt, torch_dt = _ROPE_OUT[out_dtype]
     if out is None:
-        out = torch.empty(shape, dtype=torch_dt, device=x.device)
+        out = _empty(shape, torch_dt, x.device, stream)
     elif out.dtype is not torch_dt and not (out_dtype == "fp8" and out.dtype is torch.float8_e4m3fn):
         raise JanusError(f"{what}: out is {out.dtype}, not {out_dtype}")
     xs, os_ = x.stride(), out.stride()
@@ -530,7 +544,7 @@ def rope(batch: Batch, rotary: Rotary, x, out=None, out_dtype: Optional[str] = N
         raise JanusError(f"{what}: x and out are to have one shape and adjacent elements in a head")
     if out_dtype == "fp8":
         if out_scale is None:
-            out_scale = torch.empty(total, dtype=torch.float32, device=x.device)
+            out_scale = _empty(total, torch.float32, x.device, stream)
         else:
             _want(what, "out_scale", out_scale, torch.float32, total)
     elif out_scale is not None:
@@ -566,7 +580,7 @@ def kv_append(batch: Batch, x, out, rotary: Optional[Rotary] = None, x_rot=None,
         raise JanusError(f"{what}: x, or x_rot with the elements that rotary turns, or both")
     xdt, odt = _float_code(what, "x", given), _dtype_code(out, None)
     width = out.shape[-1] if out.dim() else 0
-    if width < n or not out.is_contiguous() or out.dtype is torch.int16:
+    if width < max(n, 1) or not out.is_contiguous() or out.dtype is torch.int16:
         raise JanusError(f"{what}: out is to be contiguous rows of at least {n} elements, float32, bfloat16 or fp8")
     num_rows = out.numel() // width
     if rows is not None:
@@ -607,10 +621,10 @@ def prefix_attn(batch: Batch, q, k_pool, v_pool, page_table, page_size: int, pre
     _want(what, "page_table", page_table, torch.int32, batch.c.num_seqs, None)
     odt = {"bf16": (JANUS_BF16, torch.bfloat16), "f32": (JANUS_F32, torch.float32)}[out_dtype]
     if out is None:
-        out = torch.empty((batch.total_q, Hq, dv), dtype=odt[1], device=q.device)
+        out = _empty((batch.total_q, Hq, dv), odt[1], q.device, stream)
     _want(what, "out", out, odt[1], batch.total_q, Hq, dv)
     if want_lse and lse is None:
-        lse = torch.empty((batch.total_q, Hq), dtype=torch.float32, device=q.device)
+        lse = _empty((batch.total_q, Hq), torch.float32, q.device, stream)
     if lse is not None:
         _want(what, "lse", lse, torch.float32, batch.total_q, Hq)
     dev = _device(what, q, k_pool, v_pool, page_table, out, lse, workspace, batch.q_start)
@@ -622,7 +636,7 @@ def prefix_attn(batch: Batch, q, k_pool, v_pool, page_table, page_size: int, pre
     need = ctypes.c_size_t(0)
     _launch(what, dev, stream, lib().janus_prefix_attn, *args, None, ctypes.byref(need))
     if workspace is None:
-        workspace = torch.empty(max(int(need.value), 1), dtype=torch.uint8, device=q.device)
+        workspace = _empty(max(int(need.value), 1), torch.uint8, q.device, stream)
     have = ctypes.c_size_t(workspace.numel() * workspace.element_size())
     _launch(what, dev, stream, lib().janus_prefix_attn, *args, _at(workspace), ctypes.byref(have))
     return out, lse

@@ -129,3 +129,26 @@ def test_step_replayed():
         torch.cuda.synchronize()
         assert all(torch.equal(got[n], want[n]) for n in want)
         assert all(torch.equal(getattr(s, n), after[n]) for n in first)
+
+
+def test_what_a_call_on_another_stream_makes_belongs_to_that_stream(monkeypatch):
+    """Outputs and workspaces that a call makes itself: the allocator may give their memory to the next
+    work of the stream they were made on, which has to be the launch's."""
+    s, side, empty, streams = Layer([200, 255, 256, 391], [1, 1, 1, 1]), torch.cuda.Stream(), torch.empty, []
+    want = s.step()["dense"].clone()
+    table = s.table.clone()
+    torch.cuda.synchronize()
+
+    def seen(*args, **kw):
+        streams.append(torch.cuda.current_stream().cuda_stream)
+        return empty(*args, **kw)
+
+    monkeypatch.setattr(torch, "empty", seen)
+    janus.page_grow(s.bt, PAGE, s.free, table, stream=side)
+    janus.rope(s.bt, s.rot_i, s.qi, out_dtype="fp8", stream=side)
+    got = janus.prefix_attn(s.bt, s.q, s.kv, s.kv, s.table, PAGE, PREFIX, s.scale, dv=512, out_dtype="f32", want_lse=True,
+                            stream=side)[0]
+    monkeypatch.undo()
+    side.synchronize()
+    assert len(streams) == 2 + 2 + 3 and set(streams) == {side.cuda_stream}
+    assert torch.equal(got, want)

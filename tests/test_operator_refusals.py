@@ -200,6 +200,8 @@ def test_binding_refuses_tensors_that_do_not_fit():
         janus.kv_append(bt, x[:, 0], torch.zeros(7, 64, dtype=torch.bfloat16))  # 8 keys
     with pytest.raises(janus.JanusError):
         janus.kv_append(bt, x[:, 0], torch.zeros(10, 64, dtype=torch.bfloat16), rows=torch.zeros(3, dtype=torch.int32))
+    with pytest.raises(janus.JanusError):
+        janus.kv_append(bt, x[:, 0, :0], torch.zeros(10, 0, dtype=torch.bfloat16))      # rows of nothing
     table = torch.zeros(1, 1, dtype=torch.int32)
     with pytest.raises(janus.JanusError):
         janus.page_grow(bt, 4, torch.zeros(9, dtype=torch.int32), table)        # not on a GPU, and too narrow
