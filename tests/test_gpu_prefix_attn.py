@@ -244,3 +244,41 @@ def test_workspace_too_small():
     c = Case([20000], [1], 16, "mqa2", 0, 64)
     with pytest.raises(janus.JanusError, match="workspace too small"):
         c.run(workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))
+
+
+@pytest.mark.parametrize("kind,page", [("mla", 64), ("mla", 4), ("mqa2", 16)])
+def test_far_pages(kind, page):
+    """Rows beyond 2^32 bytes of a pool hold what rows at its beginning hold: the same result, bit by bit."""
+    c = Case([300, 333, 1000], [1, 1, 2], 16, kind, 300, page)
+    want = c.run(out_dtype="f32")
+    near = c.k.cuda()
+    width, rows = near.shape[-1], near.numel() // near.shape[-1]
+    total = -(-(5 << 30) // (2 * width)) // page * page
+    print("prefix far", kind, page, total, flush=True)
+    pools = []
+    for p in (c.k, c.v) if c.v is not c.k else (c.k,):
+        far = torch.empty((total, width), dtype=torch.bfloat16, device="cuda")
+        far[total - rows:] = p.cuda().view(rows, width)
+        pools.append(far)
+    table = torch.from_numpy(c.table).cuda()
+    table = torch.where(table >= 0, table + (total - rows) // page, table)
+    got = janus.prefix_attn(c.bt, c.q.cuda(), pools[0], pools[-1], table, page, c.prefix, float(c.scale), dv=c.dv,
+                            out_dtype="f32", want_lse=True)
+    for g, w in zip(got, want):
+        assert torch.equal(g, w)
+
+
+def test_queries_beyond_32_bits():
+    """More than 2^31 elements of q: the last sessions get what they get in a batch of their own."""
+    B, H, last = 30000, 128, 50
+    hist = np.arange(B) % 5
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    q = torch.randn((B, H, 576), generator=g, device="cuda", dtype=torch.bfloat16)
+    kv = torch.randn((64 * 16, 576), generator=g, device="cuda", dtype=torch.bfloat16)
+    table = torch.randint(0, 64, (B, 1), generator=g, device="cuda", dtype=torch.int32)
+    print("prefix many queries", q.numel(), flush=True)
+    got = janus.prefix_attn(janus.Batch(hist, [1] * B), q, kv, kv, table, 16, 0, 0.04, dv=512)[0]
+    want = janus.prefix_attn(janus.Batch(hist[-last:], [1] * last), q[-last:].contiguous(), kv, kv,
+                             table[-last:].contiguous(), 16, 0, 0.04, dv=512)[0]
+    assert q.numel() > 2**31 and torch.equal(got[-last:], want) and float(want.abs().max()) > 0.1
