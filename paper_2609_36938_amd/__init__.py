@@ -389,13 +389,14 @@ def _at(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
-def _empty(shape, dtype, device, stream):
+def _empty(dtype, device, stream, *shape):
     """A new tensor that belongs to the stream of the launch: its memory is not given to other
-    streams' work before, or after it is dropped, while that launch may use it."""
+    streams' work before, or after it is dropped, while that launch may use it.  (torch takes sizes
+    one by one faster than as a tuple.)"""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return torch.empty(*shape, dtype=dtype, device=device)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return torch.empty(*shape, dtype=dtype, device=device)
 
 
 def _launch(what: str, dev: int, stream, fn, *args):
@@ -488,8 +489,8 @@ def page_grow(batch: Batch, page_size: int, free_list, page_table, free_head=Non
     if free_head is not None and (free_head.dtype is not i32 or free_head.numel() != 1):
         raise JanusError(f"{what}: free_head is to be one int32")
     if out is None:
-        slots = _empty(total, torch.int64, page_table.device, stream)
-        counts = _empty(3, i32, page_table.device, stream)
+        slots = _empty(torch.int64, page_table.device, stream, total)
+        counts = _empty(i32, page_table.device, stream, 3)
     else:
         slots, counts = out
         _want(what, "slots", slots, torch.int64, total)
@@ -536,7 +537,7 @@ def rope(batch: Batch, rotary: Rotary, x, out=None, out_dtype: Optional[str] = N
         raise JanusError(f"{what}: unknown out_dtype {out_dtype!r}")
     odt, torch_dt = _ROPE_OUT[out_dtype]
     if out is None:
-        out = _empty(shape, torch_dt, x.device, stream)
+        out = _empty(torch_dt, x.device, stream, *shape)
     elif out.dtype is not torch_dt and not (out_dtype == "fp8" and out.dtype is torch.float8_e4m3fn):
         raise JanusError(f"{what}: out is {out.dtype}, not {out_dtype}")
     xs, os_ = x.stride(), out.stride()
@@ -544,7 +545,7 @@ def rope(batch: Batch, rotary: Rotary, x, out=None, out_dtype: Optional[str] = N
         raise JanusError(f"{what}: x and out are to have one shape and adjacent elements in a head")
     if out_dtype == "fp8":
         if out_scale is None:
-            out_scale = _empty(total, torch.float32, x.device, stream)
+            out_scale = _empty(torch.float32, x.device, stream, total)
         else:
             _want(what, "out_scale", out_scale, torch.float32, total)
     elif out_scale is not None:
@@ -610,33 +611,37 @@ def prefix_attn(batch: Batch, q, k_pool, v_pool, page_table, page_size: int, pre
     returns (out, lse or None).  q, pools, out and lse as for sparse_attn, workspace
     as for sparse_attn_split."""
     what = "janus_prefix_attn"
-    if q.dim() != 3 or q.shape[0] != batch.total_q or q.dtype != torch.bfloat16 or not q.is_contiguous():
-        raise JanusError(f"{what}: q is to be a contiguous bfloat16 [{batch.total_q}, heads, dims], not {tuple(q.shape)}")
-    Hq, dqk = int(q.shape[1]), int(q.shape[2])
-    krs = int(k_row_stride if k_row_stride is not None else k_pool.shape[-1])
-    vrs = int(v_row_stride if v_row_stride is not None else v_pool.shape[-1])
-    dv = int(dv if dv is not None else (v_pool.shape[-1] if v_pool is not k_pool else dqk))
-    if any(p.dtype != torch.bfloat16 for p in (k_pool, v_pool)) or out_dtype not in ("bf16", "f32"):
+    total, shape, bf16, dev = batch.total_q, q.shape, torch.bfloat16, q.device
+    if len(shape) != 3 or shape[0] != total or q.dtype is not bf16 or not q.is_contiguous():
+        raise JanusError(f"{what}: q is to be a contiguous bfloat16 [{total}, heads, dims], not {tuple(shape)}")
+    Hq, dqk = shape[1], shape[2]
+    krs = k_pool.shape[-1] if k_row_stride is None else int(k_row_stride)
+    vrs = v_pool.shape[-1] if v_row_stride is None else int(v_row_stride)
+    if dv is None:
+        dv = v_pool.shape[-1] if v_pool is not k_pool else dqk
+    if k_pool.dtype is not bf16 or v_pool.dtype is not bf16 or out_dtype not in ("bf16", "f32"):
         raise JanusError(f"{what}: bfloat16 pools and out_dtype bf16 or f32 expected")
     _want(what, "page_table", page_table, torch.int32, batch.c.num_seqs, None)
-    odt = {"bf16": (JANUS_BF16, torch.bfloat16), "f32": (JANUS_F32, torch.float32)}[out_dtype]
+    odt, torch_dt = (JANUS_BF16, bf16) if out_dtype == "bf16" else (JANUS_F32, torch.float32)
     if out is None:
-        out = _empty((batch.total_q, Hq, dv), odt[1], q.device, stream)
-    _want(what, "out", out, odt[1], batch.total_q, Hq, dv)
-    if want_lse and lse is None:
-        lse = _empty((batch.total_q, Hq), torch.float32, q.device, stream)
+        out = _empty(torch_dt, dev, stream, total, Hq, dv)
+    else:
+        _want(what, "out", out, torch_dt, total, Hq, dv)
     if lse is not None:
-        _want(what, "lse", lse, torch.float32, batch.total_q, Hq)
-    dev = _device(what, q, k_pool, v_pool, page_table, out, lse, workspace, batch.q_start)
-    if batch.total_q == 0:
+        _want(what, "lse", lse, torch.float32, total, Hq)
+    elif want_lse:
+        lse = _empty(torch.float32, dev, stream, total, Hq)
+    index = _device(what, q, k_pool, v_pool, page_table, out, lse, workspace, batch.q_start)
+    if total == 0:
         return out, lse
-    args = (batch.ref, _at(q), Hq, dqk, dv, _at(k_pool), _at(v_pool), krs, vrs, _at(page_table),
-            _table(batch, page_table, page_size), int(page_size), int(prefix_len), float(scale), _at(out), odt[0],
-            _at(lse))
-    need = ctypes.c_size_t(0)
-    _launch(what, dev, stream, lib().janus_prefix_attn, *args, None, ctypes.byref(need))
+    fn = lib().janus_prefix_attn
+    args = (batch.ref, q.data_ptr(), Hq, dqk, dv, k_pool.data_ptr(), v_pool.data_ptr(), krs, vrs, page_table.data_ptr(),
+            _table(batch, page_table, page_size), page_size, prefix_len, scale, out.data_ptr(), odt, _at(lse))
+    size = ctypes.c_size_t(0)
     if workspace is None:
-        workspace = _empty(max(int(need.value), 1), torch.uint8, q.device, stream)
-    have = ctypes.c_size_t(workspace.numel() * workspace.element_size())
-    _launch(what, dev, stream, lib().janus_prefix_attn, *args, _at(workspace), ctypes.byref(have))
+        _check(fn(*args, None, ctypes.byref(size), None), what)
+        workspace = _empty(torch.uint8, dev, stream, max(size.value, 1))
+    else:
+        size.value = workspace.numel() * workspace.element_size()
+    _launch(what, index, stream, fn, *args, workspace.data_ptr(), ctypes.byref(size))
     return out, lse

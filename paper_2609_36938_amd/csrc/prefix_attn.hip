@@ -74,6 +74,7 @@ struct PrefixRange {
     int row0, row1, kbeg, kend, sess;
     int64_t part;
     bool shared;
+    bool whole;  // every row has all of the keys
 };
 JANUS_DEV PrefixRange prefix_range(const PrefixArgs &g, int blk)
 {
@@ -81,11 +82,21 @@ JANUS_DEV PrefixRange prefix_range(const PrefixArgs &g, int blk)
     PrefixRange r;
     r.shared = bk.shared;
     r.sess = 0;
+    r.whole = false;
     if (bk.shared) {
         r.row0 = bk.tile * PA_ROWS;
-        r.row1 = min(r.row0 + PA_ROWS, g.q_start[g.num_seqs] * g.heads);
         r.kbeg = bk.chunk * g.plan.chunk;
         r.kend = min(r.kbeg + g.plan.chunk, g.plan.prefix);
+        const int tokens = g.q_start[g.num_seqs];
+        if (g.num_seqs <= 4 * kWave) {
+            // mostly all sessions reach behind the prefix: one load, where the search for each
+            // row's own is a chain of them
+            bool all = true;
+            for (int s = threadIdx.x & 63; s < g.num_seqs; s += kWave)
+                all = all && last_cand(g.hist_len[s], 0, g.es) + 1 >= r.kend;
+            r.whole = __ballot(!all) == 0;
+        }
+        r.row1 = min(r.row0 + PA_ROWS, tokens * g.heads);
         r.part = bk.slot * g.plan.part_rows + r.row0;
         return r;
     }
@@ -105,16 +116,9 @@ JANUS_DEV PrefixRange prefix_range(const PrefixArgs &g, int blk)
 // First key that the row's token does not attend to.
 JANUS_DEV int row_limit(const PrefixArgs &g, const PrefixRange &r, int row)
 {
+    if (r.whole)
+        return r.kend;
     const int token = row / g.heads;
-    if (r.shared && g.num_seqs <= 4 * kWave) {
-        // mostly all sessions reach behind the prefix: one load, where the search for each
-        // row's own is a chain of them
-        bool all = true;
-        for (int s = threadIdx.x & 63; s < g.num_seqs; s += kWave)
-            all = all && last_cand(g.hist_len[s], 0, g.es) + 1 >= r.kend;
-        if (__ballot(!all) == 0)
-            return r.kend;
-    }
     const int s = r.shared ? session_of_row(g.q_start, g.num_seqs, token) : r.sess;
     return min(r.kend, last_cand(g.hist_len[s], token - g.q_start[s], g.es) + 1);
 }
@@ -821,23 +825,56 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
 
 // Joins the ranges of a row: with maxima m_s and sums l_s, M = max m_s and w_s =
 // 2^(m_s - M), O = sum w_s O_s / sum w_s l_s and lse = (M + log2 sum w_s l_s) ln 2.
-// A range without keys (l = 0) wrote no O.  A worker is LANES lanes of eight dims; WPR of them
-// share a piece of a row, so that few rows of many ranges are not a chain of loads.
+// A range without keys (l = 0) wrote no O.  A worker is LANES lanes of eight dims, and WPR of
+// them share a piece of a row, each with a maximum of its own until the end, so that few
+// rows of many ranges are not a chain of loads.
 template <int DV, int LANES, int WPR>
 __global__ __launch_bounds__(256) void prefix_combine(PrefixArgs g)
 {
     constexpr int PIECES = DV / (8 * LANES), WORKERS = 256 / LANES;
     static_assert(WORKERS % WPR == 0, "whole pieces in a block");
+    // Few rows: what was not written is read as well, and not used, since a load of O that waits for
+    // its sum is another memory latency.  Many rows: that would be bytes.
+    constexpr bool FEW = WPR == 16;
     __shared__ v4f sO[WPR > 1 ? 2 * 256 : 1];
-    __shared__ float sL[WPR > 1 ? WORKERS : 1];
+    __shared__ float2 sML[WPR > 1 ? WORKERS : 1];
     const int worker = threadIdx.x / LANES, in = threadIdx.x % LANES, w = worker % WPR;
     const int slots = g.plan.slots;
     const int64_t rows = g.plan.part_rows, id = (int64_t)blockIdx.x * (WORKERS / WPR) + worker / WPR;
-    const int64_t at = id / PIECES;  // row of the workspace
+    const int64_t at = min(id / PIECES, rows - 1);  // row of the workspace
     const int dim = 8 * (LANES * (int)(id % PIECES) + in);
+    const float2 *ml = (const float2 *)(g.part + slots * rows * DV) + at;
+    const float *po = g.part + at * DV + dim;
+    const int64_t step = rows * DV;
+    float2 x[4];
+    v4f u[4], v[4];
+    auto load = [&](int s0) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int s = s0 + k * WPR;
+            x[k] = s < slots ? ml[s * rows] : float2{0.f, 0.f};
+            if (FEW) {
+                const v4f *src = (const v4f *)(po + min(s, slots - 1) * step);
+                u[k] = src[0];
+                v[k] = src[1];
+            }
+        }
+        if (!FEW) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                u[k] = v[k] = v4f{0.f, 0.f, 0.f, 0.f};
+                if (x[k].y != 0.f) {
+                    const v4f *src = (const v4f *)(po + (s0 + k * WPR) * step);
+                    u[k] = src[0];
+                    v[k] = src[1];
+                }
+            }
+        }
+    };
+    load(w);
     // the row of out that it is
-    int row = (int)min(at, rows - 1);
-    bool live = at < rows;
+    int row = (int)at;
+    bool live = id / PIECES < rows;
     if (g.plan.prefix > 0) {
         live = live && row < g.q_start[g.num_seqs] * g.heads;
     } else {
@@ -846,37 +883,18 @@ __global__ __launch_bounds__(256) void prefix_combine(PrefixArgs g)
         row = row0 + row % PA_ROWS;
         live = live && row < row1;
     }
-    const float2 *ml = (const float2 *)(g.part + slots * rows * DV) + (live ? at : 0);
-    const float *po = g.part + (live ? at : 0) * DV + dim;
-    const int64_t step = rows * DV;
-    float M = M_INIT;
-#pragma unroll 4
-    for (int s = in; s < slots; s += LANES) {
-        const float2 x = ml[s * rows];
-        M = x.y != 0.f ? fmaxf(M, x.x) : M;
-    }
-#pragma unroll
-    for (int o = 1; o < LANES; o <<= 1)
-        M = fmaxf(M, __shfl_xor(M, o));
-    float L = 0.f;
+    float M = M_INIT, L = 0.f;
     v4f a = {0.f, 0.f, 0.f, 0.f}, b = a;
-    for (int s0 = w; s0 < slots; s0 += 4 * WPR) {
-        float2 x[4];
-        v4f u[4], v[4];
+    for (int s0 = w;;) {
+        float top = M;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int s = s0 + k * WPR;
-            x[k] = s < slots ? ml[s * rows] : float2{0.f, 0.f};
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            u[k] = v[k] = v4f{0.f, 0.f, 0.f, 0.f};
-            if (x[k].y != 0.f) {
-                const v4f *src = (const v4f *)(po + (s0 + k * WPR) * step);
-                u[k] = src[0];
-                v[k] = src[1];
-            }
-        }
+        for (int k = 0; k < 4; ++k)
+            top = x[k].y != 0.f ? fmaxf(top, x[k].x) : top;
+        const float old = __builtin_amdgcn_exp2f(M - top);
+        M = top;
+        L *= old;
+        a *= old;
+        b *= old;
 #pragma unroll
         for (int k = 0; k < 4; ++k)
             if (x[k].y != 0.f) {
@@ -885,20 +903,34 @@ __global__ __launch_bounds__(256) void prefix_combine(PrefixArgs g)
                 a += f * u[k];
                 b += f * v[k];
             }
+        s0 += 4 * WPR;
+        if (s0 >= slots)
+            break;
+        load(s0);
     }
     if constexpr (WPR > 1) {
         sO[2 * threadIdx.x] = a;
         sO[2 * threadIdx.x + 1] = b;
         if (in == 0)
-            sL[worker] = L;
+            sML[worker] = float2{M, L};
         __syncthreads();
         if (w != 0)
             return;
+        float2 y[WPR];
 #pragma unroll
-        for (int k = 1; k < WPR; ++k) {
-            a += sO[2 * (threadIdx.x + k * LANES)];
-            b += sO[2 * (threadIdx.x + k * LANES) + 1];
-            L += sL[worker + k];
+        for (int k = 0; k < WPR; ++k)
+            y[k] = sML[worker + k];
+#pragma unroll
+        for (int k = 1; k < WPR; ++k)
+            M = fmaxf(M, y[k].x);
+        L = 0.f;
+        a = b = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int k = 0; k < WPR; ++k) {  // (a worker without keys: sums of 0)
+            const float f = __builtin_amdgcn_exp2f(y[k].x - M);
+            L += f * y[k].y;
+            a += f * sO[2 * (threadIdx.x + k * LANES)];
+            b += f * sO[2 * (threadIdx.x + k * LANES) + 1];
         }
     }
     if (!live)
