@@ -1,19 +1,29 @@
 // Dense causal attention over the paged cache, for a batch whose sessions
 // begin with a common prefix.
 //
-// A row is one (token, head).  A block takes 128 rows and a range of keys and
-// goes over them once with a running maximum and sum (exp2 domain):
-//   * 32 or 64 keys at a time come straight into LDS (global_load_lds), into a
-//     ring of tile buffers.  Within a row the 16-byte chunks are exchanged by the
-//     row's number (swz), so that neither the row-wise reads of K nor the
-//     transposing reads of V meet in a bank.
-//   * A wave has 32 of the rows: their queries in registers, S^T = K Q^T on
-//     32x32x16 MFMA.  A lane's results then are one row's logits, and the
-//     exponentials, as they lie, the operand of O^T = V^T P^T: probabilities
-//     never leave the lane, and rescaling O needs no exchange.
+// A row is one (token, head): o = sum_j 2^(x_j - m) v_j / sum_j 2^(x_j - m), with
+// x_j = (q . k_j) scale log2 e over the keys before the row's limit.  A block takes
+// 128 rows and a range of keys and goes over them once, in tiles of 32:
+//   * The tiles come straight into LDS (global_load_lds), into a ring of buffers two or
+//     three tiles ahead.  Within a row the 16-byte chunks are exchanged by the row's
+//     number (swz16, swz8): neither the row-wise reads of K nor the transposing
+//     reads of V meet in a bank (0 conflict cycles counted).
+//   * A wave has 32 of the rows and scores them: their queries in registers, S^T = K Q^T
+//     on 32x32x16 MFMA, so that a lane's results are logits of one row and
+//     its exponentials, as they lie, are the operand of O^T = V^T P^T.
 //   * Rows of different sessions share the blocks over the prefix: its keys are
 //     read once for 128 rows instead of once for each session's heads.
-// Ranges of one row are joined by their maxima and sums (prefix_combine).
+//   * Ranges of one row are joined by their maxima and sums (prefix_combine): few rows
+//     have too few blocks for 256 CUs otherwise.
+// Logits, maxima, sums and O are fp32.  Probabilities are rounded to bf16, the type of
+// the V that they multiply; their sums are taken before that.  The error is 2^-9 of the
+// values at most for each key, and mostly averages out (2.2e-3 of the result
+// with 4096 keys, 1.7e-3 of it the rounding of the result to bf16).
+//
+// Two kernels, by what a row costs in registers.  prefix_mqa: 128 dims, O of a wave's own rows
+// in its registers, two blocks a CU.  prefix_mla: O of 128 rows of 512 dims is all
+// the accumulators of a CU, so a wave has a quarter of the dims of all rows, and the
+// probabilities go through LDS.
 #include "attn_device.hpp"
 #include "janus_device.hpp"
 #include "janus_host.hpp"
@@ -198,6 +208,16 @@ JANUS_DEV int swz8(int r) { return ((r & 2) << 1) | ((r & 4) >> 1) | ((r & 8) >>
 
 constexpr int PQ_KT = 32;  // keys of a tile
 
+// MQA, 128 dims.  A tile is 8 MFMAs for S^T and 8 for O^T in each wave, 512 cycles, and
+// 16 exponentials a lane: those go under the MFMAs that score the next tile.  What bounds
+// it: long contexts, the MFMAs and what is not under them (2 sessions of 1000 to
+// 2000 tokens x 16 heads on 31000 ids: 775 to 810 us, 1.0 PFLOP/s; scores and exponentials one after
+// the other 10% more); few rows, the chain of loads before the first tile (2.4 us), a loop of
+// few tiles, and the launch of the join (16 sessions x 8 heads on 4096 ids: 10.5 of
+// 13.8 us).  32 keys a tile and 66 KB of LDS let two blocks share a CU, so that one's
+// waits are the other's work: the first form took 1740 us for the long case with 64 keys
+// and one block a CU, 1190 with this.  Four buffers, and a turn for each of them, keep
+// LDS offsets constant.
 __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
 {
     constexpr int RB = 256;                              // bytes of a row
@@ -467,6 +487,21 @@ JANUS_DEV void mfma_next(v16f &s, v4i a, v8bf b)
 }
 JANUS_DEV void settled(v16f &s) { asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s)); }
 
+// MLA, 576 dims scored and 512 of them multiplied again as V.  A wave scores its 32 rows (36 MFMAs,
+// a chain), writes their probabilities to LDS, and multiplies all 128 rows' by its 128
+// dims of V (32 MFMAs): V is read from LDS once a block instead of once a wave, and O^T takes 256
+// accumulators, which leaves 256 registers for 144 of queries and the operands.
+// While tile t is scored, tile t - 1 is multiplied: PM_WITH of its steps stand among the chain's, the
+// others under the exponentials (the longest case below 7.77 ms with 8 steps, 7.40 with 16, 7.43 with
+// 24, on one box).  What bounds it is the rate of the MFMAs at the power the chip has: 1.16 to
+// 1.22 PFLOP/s on long ranges (8 sessions of 100 to 300 tokens x 128 heads on 17000 ids, 6.6 to
+// 6.9 ms), where a library product of 8192^3 reaches 1.22 and of 16384^3 1.40; they are busy in
+// 55% of the cycles.  Few rows pay 5 to 8 us before the first tile (queries and tiles from HBM), as
+// much behind the last, and the join: 32 sessions x 16 heads on 131072 ids take 170 us where
+// the product's rate would take 105.  The first form, with each wave's O^T rescaled
+// as maxima grow, spilled it and took 95 ms for the longest case; gathers left out behind the last
+// tile, by a branch, cost 7%.
+// SMALL: pages of fewer than eight ids, where a wave's eight rows lie in different ones.
 template <bool SMALL>
 __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
 {
@@ -825,9 +860,12 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
 
 // Joins the ranges of a row: with maxima m_s and sums l_s, M = max m_s and w_s =
 // 2^(m_s - M), O = sum w_s O_s / sum w_s l_s and lse = (M + log2 sum w_s l_s) ln 2.
-// A range without keys (l = 0) wrote no O.  A worker is LANES lanes of eight dims, and WPR of
-// them share a piece of a row, each with a maximum of its own until the end, so that few
-// rows of many ranges are not a chain of loads.
+// A range without keys (l = 0) wrote no O.  Bound by bytes where rows are many (22528 rows
+// of six ranges of 512 dims: 285 MB read in 71 us, 4.0 TB/s), by latency where they are few (128
+// rows of 72 ranges of 128 dims: 3.9 us; with the maxima of all ranges first, which O's loads
+// waited for, 6.3).  A worker is LANES lanes of eight dims, and WPR of them share a piece of a row, each with a
+// maximum of its own until the end, so that few rows of many ranges are not a chain of loads (with
+// one worker a row, 69 ranges took 55 us).
 template <int DV, int LANES, int WPR>
 __global__ __launch_bounds__(256) void prefix_combine(PrefixArgs g)
 {
@@ -952,9 +990,15 @@ static void launch_combine(const PrefixArgs &g, hipStream_t st)
     };
     using std::integral_constant;
     constexpr int ALL = DV / 8;  // lanes of a whole row
-    if (g.plan.slots <= 4)  // a worker has all of a row's ranges in flight at once
+    // A worker a row keeps four ranges in flight.  Few rows: sixteen workers and a block each, or to each
+    // quarter of one.  Calls with four workers against these two: 8192 rows of 4 ranges of 512 dims 579 us
+    // and 570, of 7.5 ranges of 128 dims 62.1 and 58.7, 1024 rows of 24 ranges of 128 dims 24.7 and 27.2;
+    // 128 rows of 228 ranges of 512 dims 60.3 and 52.9, of 72 ranges of 128 dims 17.1 and 14.0,
+    // 512 rows of 61 ranges of 512 dims 66.9 and 68.7, 2048 rows of 24 ranges of 128 dims 47.4 and 50.7.
+    const bool few = g.plan.part_rows * DV < 1 << 17;
+    if (g.plan.slots <= (few ? 4 : 16))
         go(integral_constant<int, ALL>{}, integral_constant<int, 1>{});
-    else if (g.plan.part_rows * (DV / 128) <= (DV == 512 ? 512 : 4096))  // few rows: a block each, or to each quarter of one
+    else if (few)
         go(integral_constant<int, 16>{}, integral_constant<int, 16>{});
     else
         go(integral_constant<int, ALL>{}, integral_constant<int, 4>{});

@@ -15,7 +15,13 @@
 // length of its row): an fp8 row's largest value is then a reduction over
 // those lanes, and short rows share a block.  A lane's unit is two groups of V
 // elements: the two halves of V pairs that lie apart, or 2 V neighbours.  Loads go out before the
-// angles are worked out.  Bound by the bytes read and written.
+// angles are worked out.
+//
+// Bound by the bytes read and written where there are many (8192 tokens x 128 heads x 64 rotated
+// dims of bf16, 268 MB: 59 us, 4.5 TB/s; 2048 tokens x 64 heads x 128 dims to fp8, 50 MB: 11.2 us),
+// by one chain of loads (the session, its length, the frequencies' angles, the slot) where there are
+// few (16 decode queries 3.7 us, 64 cache rows to fp8 4.2; an empty kernel takes 2.5).  Loads behind
+// branches, which wait for each other: 71 us for the first of these.
 #include "janus_device.hpp"
 #include "janus_host.hpp"
 
@@ -380,8 +386,8 @@ static void launch_rope_rows(RopeArgs g, hipStream_t st)
                            dim3(ROPE_THREADS), (size_t)rows * (g.dim / 2) * sizeof(float2), st, g);
     };
     // Many rows: the fewest lanes whose registers hold one, since a lane takes as many
-    // instructions whether or not it has a unit (8192 MLA rows, 36 units of 16 elements, 6.6 us
-    // on 16 lanes of three units, 7.4 on 64 lanes of two).  Few rows: one unit a lane (64 of them 4.6 us, 5.6).
+    // instructions whether or not it has a unit (8192 MLA rows, 36 units of 16 elements, 6.5 us
+    // on 16 lanes of three units, 7.3 on 64 lanes of two).  Few rows: one unit a lane (64 of them 4.2 us, 4.6 with two).
     using std::integral_constant;
     if (V > 1 && units <= 16)
         go(integral_constant<int, 16>{}, integral_constant<int, 1>{});
