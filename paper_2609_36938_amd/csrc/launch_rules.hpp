@@ -218,10 +218,10 @@ constexpr PrefixPlan prefix_plan(int num_seqs, int total_q, int max_ctx, int64_t
     // empty ones are not all taken again.  Without them counted, up to 4/5.)  An MQA
     // block beside another on its CU adds a third of its time.  Each block starts for 64 keys,
     // and a range of a row costs a hundredth of a key to write and read again.  Fitted
-    // to 35 batches of 1 to 100 sessions, each with 27 chunk lengths; of 24 of them, timed again
-    // on the kernels as they are, the chunk taken is 0.1% off the best one in the mean for
-    // MLA and 3.5% for MQA, 11% at most (whole rounds of blocks, a start of 128 or
-    // 256 keys and a join of 0.02 or 0.01: 6 and 13% in the mean of the first 18).
+    // to 35 batches of 1 to 100 sessions; of 39 batches on the kernels as they are, each with 27
+    // chunk lengths, the chunk taken is 0.5% off the best one in the mean for MLA and
+    // 2.6% for MQA, 10% at most (whole rounds of blocks, a start of 128 or 256 keys and a
+    // join of 0.02 or 0.01: 6 and 13% in the mean of the first 18).
     const double start = 64, join = 0.01, tail = 0.5, slack = 0.8, beside = mla ? 0.0 : 0.35;
     const double room = (mla && heads % PA_ROWS != 0 ? 0.94 : 1.0) * resident;
     double best = -1.0;

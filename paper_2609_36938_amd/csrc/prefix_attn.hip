@@ -213,11 +213,10 @@ constexpr int PQ_KT = 32;  // keys of a tile
 // it: long contexts, the MFMAs and what is not under them (2 sessions of 1000 to
 // 2000 tokens x 16 heads on 31000 ids: 775 to 810 us, 1.0 PFLOP/s; scores and exponentials one after
 // the other 10% more); few rows, the chain of loads before the first tile (2.4 us), a loop of
-// few tiles, and the launch of the join (16 sessions x 8 heads on 4096 ids: 10.5 of
-// 13.8 us).  32 keys a tile and 66 KB of LDS let two blocks share a CU, so that one's
-// waits are the other's work: the first form took 1740 us for the long case with 64 keys
-// and one block a CU, 1190 with this.  Four buffers, and a turn for each of them, keep
-// LDS offsets constant.
+// few tiles, and the launch of the join (16 sessions x 8 heads on 4096 ids: 10.4 us).  32
+// keys a tile and 66 KB of LDS let two blocks share a CU, so that one's waits are the
+// other's work: the first form took 1740 us for the long case with 64 keys and one block a
+// CU, 1190 with this.  Four buffers, and a turn for each of them, keep LDS offsets constant.
 __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
 {
     constexpr int RB = 256;                              // bytes of a row
@@ -861,11 +860,11 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
 // Joins the ranges of a row: with maxima m_s and sums l_s, M = max m_s and w_s =
 // 2^(m_s - M), O = sum w_s O_s / sum w_s l_s and lse = (M + log2 sum w_s l_s) ln 2.
 // A range without keys (l = 0) wrote no O.  Bound by bytes where rows are many (22528 rows
-// of six ranges of 512 dims: 285 MB read in 71 us, 4.0 TB/s), by latency where they are few (128
-// rows of 72 ranges of 128 dims: 3.9 us; with the maxima of all ranges first, which O's loads
-// waited for, 6.3).  A worker is LANES lanes of eight dims, and WPR of them share a piece of a row, each with a
-// maximum of its own until the end, so that few rows of many ranges are not a chain of loads (with
-// one worker a row, 69 ranges took 55 us).
+// of six ranges of 512 dims, 305 MB: 50 us, 6.1 TB/s), by latency where they are few (128 rows of
+// 72 ranges of 128 dims: 4.2 us; with the maxima of all ranges first, which O's loads waited
+// for, 6.3).  A worker is LANES lanes of eight dims, and WPR of them share a piece of a
+// row, each with a maximum of its own until the end, so that few rows of many ranges are
+// not a chain of loads (with one worker a row, 69 ranges took 55 us).
 template <int DV, int LANES, int WPR>
 __global__ __launch_bounds__(256) void prefix_combine(PrefixArgs g)
 {
