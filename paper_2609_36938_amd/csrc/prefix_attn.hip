@@ -492,7 +492,7 @@ JANUS_DEV void settled(v16f &s) { asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s));
 // accumulators, which leaves 256 registers for 144 of queries and the operands.
 // While tile t is scored, tile t - 1 is multiplied: PM_WITH of its steps stand among the chain's, the
 // others under the exponentials (the longest case below 7.77 ms with 8 steps, 7.40 with 16, 7.43 with
-// 24, on one box).  What bounds it is the rate of the MFMAs at the power the chip has: 1.16 to
+// 24, on one card).  What bounds it is the rate of the MFMAs at the power the chip has: 1.16 to
 // 1.22 PFLOP/s on long ranges (8 sessions of 100 to 300 tokens x 128 heads on 17000 ids, 6.6 to
 // 6.9 ms), where a library product of 8192^3 reaches 1.22 and of 16384^3 1.40; they are busy in
 // 55% of the cycles.  Few rows pay 5 to 8 us before the first tile (queries and tiles from HBM), as
@@ -592,6 +592,7 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
     if (nt > 0) {
         issue(0);
         issue(1);
+        issue(2);
     }
 
     const int kcol = (hf ^ swz16(c32)) * 16, tcol = (hf ^ swz8(c32)) * 16;
@@ -599,7 +600,7 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
     const int vch = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
     v16f s;
     v8bf pb[2];
-    landed();
+    __builtin_amdgcn_s_waitcnt(vmcnt_only(18));
     lds_barrier();
     int bmin;  // keys before it are every row's of the block
     {
@@ -741,7 +742,6 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
                     for (int i = 0; i < 16; ++i)
                         o[d][rb][i] = 0.f;
             lsum = 0.f;
-            issue(2);
             logits(0, std::integral_constant<int, 0>{}, 0);
             probabilities(mask(0));
             give(0);
@@ -804,7 +804,8 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
             lds_barrier();
             issue(0);
             issue(1);
-            landed();
+            issue(2);
+            __builtin_amdgcn_s_waitcnt(vmcnt_only(18));
             lds_barrier();
         }
         __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
