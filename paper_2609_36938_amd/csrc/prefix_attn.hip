@@ -16,7 +16,7 @@
 //   * Ranges of one row are joined by their maxima and sums (prefix_combine): few rows
 //     have too few blocks for 256 CUs otherwise.
 // Logits, maxima, sums and O are fp32.  Probabilities are rounded to bf16, the type of
-// the V that they multiply; their sums are taken before that.  The error is 2^-9 of the
+// the V that they multiply; their sums are taken before that.  The error is 2^-8 of the
 // values at most for each key, and mostly averages out (2.2e-3 of the result
 // with 4096 keys, 1.7e-3 of it the rounding of the result to bf16).
 //

@@ -282,3 +282,17 @@ def test_queries_beyond_32_bits():
     want = janus.prefix_attn(janus.Batch(hist[-last:], [1] * last), q[-last:].contiguous(), kv, kv,
                              table[-last:].contiguous(), 16, 0, 0.04, dv=512)[0]
     assert q.numel() > 2**31 and torch.equal(got[-last:], want) and float(want.abs().max()) > 0.1
+
+
+@pytest.mark.parametrize("kind,hist,new", [("mla", [300], [70]), ("mla", [5000], [1]), ("mqa2", [300], [70]), ("mqa2", [5000], [1])])
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_outputs_at_four_bytes(kind, hist, new, dt):
+    """An output that begins at any word: the results of an aligned one, and nothing before or behind them."""
+    c = Case(hist, new, 16, kind, 0, 64)
+    want, lse = c.run(out_dtype=dt)
+    skip = 2 if dt == "bf16" else 1
+    buf = torch.full((want.numel() + 2 * skip,), 7, dtype=want.dtype, device="cuda")
+    lbuf = torch.full((lse.numel() + 2,), 7, dtype=torch.float32, device="cuda")
+    out, got = c.run(out_dtype=dt, out=buf[skip:-skip].view(want.shape), lse=lbuf[1:-1].view(lse.shape))
+    assert torch.equal(out, want) and torch.equal(got, lse)
+    assert (buf[:skip] == 7).all() and (buf[-skip:] == 7).all() and lbuf[0] == 7 and lbuf[-1] == 7

@@ -5,6 +5,8 @@ With k at least the context the selection is everything, so sparse_attn and pref
 is held to the 64-bit form of the cache's own contents (read back), prefix_attn by its derived tolerance and the path's
 calls by theirs (2e-2, absolute and of the row's largest output).  The cache's contents themselves are held to the
 formula by the operators' own tests."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -152,3 +154,32 @@ def test_what_a_call_on_another_stream_makes_belongs_to_that_stream(monkeypatch)
     side.synchronize()
     assert len(streams) == 2 + 2 + 3 and set(streams) == {side.cuda_stream}
     assert torch.equal(got, want)
+
+
+def test_two_threads_on_streams_of_their_own():
+    """Two sessions' steps at once: no call keeps anything that another one's could meet."""
+    layers = [Layer([200, 255, 256, 391], [1, 1, 1, 1]), Layer([200, 300, 210], [70, 1, 33], seed=1)]
+    first = [{n: getattr(s, n).clone() for n in ("table", "kv", "kv8", "keys", "kscale", "q")} for s in layers]
+    want = [{n: t.clone() for n, t in s.step().items()} for s in layers]
+    torch.cuda.synchronize()
+    streams, got, wrong = [torch.cuda.Stream() for _ in layers], [None, None], []
+
+    def work(i):
+        try:
+            with torch.cuda.stream(streams[i]):
+                for _ in range(20):
+                    for n, t in first[i].items():
+                        getattr(layers[i], n).copy_(t)
+                    got[i] = layers[i].step()
+                streams[i].synchronize()
+        except Exception as e:  # (of the thread: told by the test)
+            wrong.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong, wrong
+    for i in range(2):
+        assert all(torch.equal(got[i][n], want[i][n]) for n in want[i])
