@@ -296,3 +296,25 @@ def test_outputs_at_four_bytes(kind, hist, new, dt):
     out, got = c.run(out_dtype=dt, out=buf[skip:-skip].view(want.shape), lse=lbuf[1:-1].view(lse.shape))
     assert torch.equal(out, want) and torch.equal(got, lse)
     assert (buf[:skip] == 7).all() and (buf[-skip:] == 7).all() and lbuf[0] == 7 and lbuf[-1] == 7
+
+
+@pytest.mark.parametrize("kind", ["mla", "mqa2"])
+def test_replays_with_shorter_sessions(kind):
+    """A captured call reads the lengths on the device: up to those it was made for, each replay has the lengths
+    of its time."""
+    c = Case([900, 1500, 700], [1, 2, 1], 16, kind, 500, 64)
+    args = (c.q.cuda(), *(t.cuda() for t in (c.k, c.v)), torch.from_numpy(c.table).cuda(), 64, 500, float(c.scale))
+    if c.v is c.k:
+        args = (args[0], args[1], args[1], *args[3:])
+    call = lambda bt: janus.prefix_attn(bt, *args, dv=c.dv, out_dtype="f32", want_lse=True)  # noqa: E731
+    call(c.bt)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, lse = call(c.bt)
+    for hist in ([900, 1500, 700], [501, 640, 500], [899, 64, 0]):
+        c.bt.hist_len.copy_(torch.tensor(hist, dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        c.hist = hist
+        c.check(out, lse)
