@@ -133,6 +133,23 @@ JANUS_DEV int row_limit(const PrefixArgs &g, const PrefixRange &r, int row)
     return min(r.kend, last_cand(g.hist_len[s], token - g.q_start[s], g.es) + 1);
 }
 
+// Keys before it are every row's of the block, whose limits are in LDS.  One session's grow with its
+// rows; only where sessions end inside the prefix are all of them looked at.
+JANUS_DEV int block_limit(const PrefixRange &r, const int *lim)
+{
+    if (r.whole)
+        return r.kend;
+    if (!r.shared)
+        return __builtin_amdgcn_readfirstlane(lim[0]);
+    const int lane = threadIdx.x & 63;
+    int least = min(r.row0 + lane < r.row1 ? lim[lane] : 0x7fffffff,
+                    r.row0 + 64 + lane < r.row1 ? lim[64 + lane] : 0x7fffffff);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1)
+        least = min(least, __shfl_xor(least, o));
+    return __builtin_amdgcn_readfirstlane(least);
+}
+
 // The block's rows without matrix instructions: a wave a row, a lane a key, then DV / 64 dims.
 // For blocks that hold an infinity or NaN in a row of V of a tile in which rows end
 // at different keys: a probability of 0 does not undo it for the rows without the key.
@@ -239,12 +256,6 @@ __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
     const int lim = row_limit(g, r, live ? row : r.row1 - 1);
     if (hf == 0)
         sLim[32 * wave + c32] = lim;
-    int wmin = live ? lim : 0x7fffffff;  // keys before it are every row's of the wave
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1)
-        wmin = min(wmin, __shfl_xor(wmin, o));
-    wmin = __builtin_amdgcn_readfirstlane(wmin);
-
     v8bf qf[STEPS];
     {
         const uint16_t *qr = g.q + (int64_t)(live ? row : r.row1 - 1) * 128 + 8 * hf;
@@ -259,7 +270,8 @@ __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
         for (int i = 0; i < 16; ++i)
             o[d][i] = 0.f;
     float m = M_INIT, lsum = 0.f;
-    int bad = 0;  // a tile where rows end holds values of V that are not finite
+    int bad = 0;   // a tile where rows end holds values of V that are not finite
+    int bmin = 0;  // keys before it are every row's
 
     // Tiles begin at multiples of their length: a tile of longer pages lies in one.
     // A wave gathers four rows at a time, rows 16 j + 4 wave .. of K and of V.
@@ -338,7 +350,7 @@ __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
         const uint8_t *vt = ring + SLOT * BUF + KBUF;
         const int base = base0 + t * PQ_KT;
         float mult = g.scale_log2;
-        if (base < kbeg || base + PQ_KT > wmin || mult <= 0.f) {
+        if (base < kbeg || base + PQ_KT > bmin || mult <= 0.f) {
             // keys 8 (i / 4) + 4 hf + i % 4 of this lane's row
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -346,9 +358,9 @@ __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
                 s[i] = key >= kbeg && key < lim ? s[i] * mult : -INFINITY;
             }
             mult = 1.f;
-#pragma unroll 1
-            for (int w = 0; w < KBUF / 1024; ++w) {
-                const v4i x = *(const v4i *)(vt + 1024 * w + 16 * lane);
+#pragma unroll
+            for (int w = 0; w < KBUF / 1024; w += PA_WAVES) {  // (every wave comes here)
+                const v4i x = *(const v4i *)(vt + 1024 * (w + wave) + 16 * lane);
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     bad |= (x[e] & 0x7f80) == 0x7f80 || (x[e] & 0x7f800000) == 0x7f800000;
@@ -413,6 +425,7 @@ __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
         using std::integral_constant;
         __builtin_amdgcn_s_waitcnt(vmcnt_only(4 * GATHERS));
         lds_barrier();
+        bmin = block_limit(r, sLim);
         v16f sa = logits(ring), sb;
 #pragma unroll 1
         for (int t = 0;; t += 4) {
@@ -602,16 +615,7 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
     v8bf pb[2];
     __builtin_amdgcn_s_waitcnt(vmcnt_only(18));
     lds_barrier();
-    int bmin;  // keys before it are every row's of the block
-    {
-        const int a = r.row0 + lane < r.row1 ? sLim[lane] : 0x7fffffff;
-        const int b = r.row0 + 64 + lane < r.row1 ? sLim[64 + lane] : 0x7fffffff;
-        bmin = min(a, b);
-#pragma unroll
-        for (int x = 1; x < 64; x <<= 1)
-            bmin = min(bmin, __shfl_xor(bmin, x));
-        bmin = __builtin_amdgcn_readfirstlane(bmin);
-    }
+    const int bmin = block_limit(r, sLim);
     int bad = 0;  // a tile where rows end holds values of V that are not finite
 
     // O += P V of a tile, this wave's dims, as 32 steps: keys 16 h + .., dims 128 wave +
