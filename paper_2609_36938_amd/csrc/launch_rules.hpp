@@ -184,6 +184,7 @@ struct PrefixPlan {
     int chunk;         // keys of a block
     int shared_tiles, shared_chunks;  // over the prefix
     int own_tiles, own_chunks;        // over the ids behind it
+    int one;           // no session has more than a tile: tile s is session s
     int whole;         // own tiles, the first ones, that are one block each over all their keys
     int alike;         // own chunks that read the same pages in every session
     int slots;         // ranges of a row whose keys are split (1: none is)
@@ -191,8 +192,8 @@ struct PrefixPlan {
     int64_t blocks;
 };
 
-constexpr PrefixPlan prefix_plan(int num_seqs, int total_q, int max_ctx, int64_t total_ctx, int prefix_len, int heads,
-                                 bool mla)
+constexpr PrefixPlan prefix_plan(int num_seqs, int total_q, int max_q, int max_ctx, int64_t total_ctx, int prefix_len,
+                                 int heads, bool mla)
 {
     PrefixPlan p = {};
     const int64_t rows = (int64_t)total_q * heads;
@@ -204,7 +205,11 @@ constexpr PrefixPlan prefix_plan(int num_seqs, int total_q, int max_ctx, int64_t
     const int tile = 32, resident = PA_CUS * (mla ? 1 : 2);
     p.prefix = share ? prefix_len : 0;
     p.shared_tiles = share ? full : 0;
-    p.own_tiles = prefix_tile_first(total_q, heads, num_seqs);
+    // Tiles by session where none has more than one: with tiles that may be empty, either some CUs have
+    // no block or more blocks than the chip takes at once do have rows (64 sessions of 64 MLA heads
+    // on a prefix of 16384 201 us, by session 167; 32 of 32 heads on 65536 170 and 162).
+    p.one = heads % PA_ROWS != 0 && (int64_t)max_q * heads <= PA_ROWS;
+    p.own_tiles = p.one ? num_seqs : prefix_tile_first(total_q, heads, num_seqs);
     // Whole rounds of blocks need no split; the last tiles are split over the round that is left.
     const int64_t rounds = share ? 0 : apart / resident;
     p.whole = (int)(rounds * resident * p.own_tiles / apart);
@@ -223,9 +228,9 @@ constexpr PrefixPlan prefix_plan(int num_seqs, int total_q, int max_ctx, int64_t
     // 2.6% for MQA, 10% at most (whole rounds of blocks, a start of 128 or 256 keys and a
     // join of 0.02 or 0.01: 6 and 13% in the mean of the first 18).
     const double start = 64, join = 0.01, tail = 0.5, slack = 0.8, beside = mla ? 0.0 : 0.35;
-    const double room = (mla && heads % PA_ROWS != 0 ? 0.94 : 1.0) * resident;
+    const double room = (mla && heads % PA_ROWS != 0 && !p.one ? 0.94 : 1.0) * resident;
     double best = -1.0;
-    for (int n = 1; n <= 256; n += 1 + n / 16) {
+    auto attempt = [&](int n) {  // n chunks over the longer part; whether more would be too many
         const int chunk = (span > n ? (span + n - 1) / n + tile - 1 : tile) / tile * tile;
         const int sc = share ? (prefix_len + chunk - 1) / chunk : 0, oc = own > 0 ? (own + chunk - 1) / chunk : 1;
         const int mine = mean > 0 ? (mean + chunk - 1) / chunk : 1;
@@ -247,9 +252,14 @@ constexpr PrefixPlan prefix_plan(int num_seqs, int total_q, int max_ctx, int64_t
             p.shared_chunks = sc;
             p.own_chunks = oc;
         }
-        if (chunk == tile || work > 8.0 * resident)
-            break;
-    }
+        return chunk == tile || work > 8.0 * resident;
+    };
+    for (int n = 1; n <= 256 && !attempt(n); n += 1 + n / 16)
+        ;
+    // and as many as fill the chip once, with the own chunks as they are
+    const double fill = share ? (room - (double)ids * p.own_chunks) / p.shared_tiles : room / (double)(ids > 0 ? ids : 1);
+    if (fill > 1.0)
+        attempt((int)fill);
     p.slots = p.shared_chunks + p.own_chunks;
     if (p.slots == 1 || rest == 0) {
         p.whole = p.own_tiles;

@@ -60,6 +60,11 @@ struct PrefixArgs {
 template <bool WAVE>
 JANUS_DEV int tile_rows(const PrefixArgs &g, int tile, int &row0, int &row1)
 {
+    if (g.plan.one) {
+        row0 = g.q_start[tile] * g.heads;
+        row1 = min(row0 + PA_ROWS, g.q_start[tile + 1] * g.heads);
+        return tile;
+    }
     int lo = 0, hi = g.num_seqs;  // the session is in [lo, hi)
     while (hi - lo > 1) {
         if constexpr (WAVE) {
@@ -1031,7 +1036,7 @@ extern "C" int janus_prefix_attn(const janus_batch *bt, const void *q, int Hq, i
         (int64_t)bt->total_q * Hq + (int64_t)bt->num_seqs * PA_ROWS >= (int64_t)1 << 31)
         return JANUS_ERR_UNSUPPORTED;
     const PrefixPlan plan =
-        prefix_plan(bt->num_seqs, bt->total_q, bt->max_ctx, bt->total_ctx, prefix_len, Hq, mla);
+        prefix_plan(bt->num_seqs, bt->total_q, bt->max_q, bt->max_ctx, bt->total_ctx, prefix_len, Hq, mla);
     if (plan.blocks > PA_MAX_BLOCKS)
         return JANUS_ERR_UNSUPPORTED;
     const size_t need = plan.slots > 1 ? (size_t)plan.slots * plan.part_rows * (dv + 2) * sizeof(float) : 0;

@@ -11,17 +11,17 @@ CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
 WRAP = r"""
 #include "launch_rules.hpp"
 using namespace janus;
-extern "C" void plan(int n, int total_q, int max_ctx, long total_ctx, int prefix, int heads, int mla, long *o)
+extern "C" void plan(int n, int total_q, int max_q, int max_ctx, long total_ctx, int prefix, int heads, int mla, long *o)
 {
-    const PrefixPlan p = prefix_plan(n, total_q, max_ctx, total_ctx, prefix, heads, mla);
+    const PrefixPlan p = prefix_plan(n, total_q, max_q, max_ctx, total_ctx, prefix, heads, mla);
     const long v[] = {p.prefix, p.chunk, p.shared_tiles, p.shared_chunks, p.own_tiles, p.own_chunks, p.whole, p.alike,
-                      p.slots, (long)p.part_rows, (long)p.blocks};
-    for (int i = 0; i < 11; ++i)
+                      p.slots, (long)p.part_rows, (long)p.blocks, p.one};
+    for (int i = 0; i < 12; ++i)
         o[i] = v[i];
 }
-extern "C" void blocks(int n, int total_q, int max_ctx, long total_ctx, int prefix, int heads, int mla, int *o)
+extern "C" void blocks(int n, int total_q, int max_q, int max_ctx, long total_ctx, int prefix, int heads, int mla, int *o)
 {
-    const PrefixPlan p = prefix_plan(n, total_q, max_ctx, total_ctx, prefix, heads, mla);
+    const PrefixPlan p = prefix_plan(n, total_q, max_q, max_ctx, total_ctx, prefix, heads, mla);
     for (int b = 0; b < p.blocks; ++b) {
         const PrefixBlock k = prefix_block(p, b);
         o[4 * b] = k.shared, o[4 * b + 1] = k.tile, o[4 * b + 2] = k.chunk, o[4 * b + 3] = k.slot;
@@ -29,7 +29,7 @@ extern "C" void blocks(int n, int total_q, int max_ctx, long total_ctx, int pref
 }
 extern "C" int first(int q, int heads, int s) { return prefix_tile_first(q, heads, s); }
 """
-NAMES = "prefix chunk shared_tiles shared_chunks own_tiles own_chunks whole alike slots part_rows blocks".split()
+NAMES = "prefix chunk shared_tiles shared_chunks own_tiles own_chunks whole alike slots part_rows blocks one".split()
 
 
 @pytest.fixture(scope="module")
@@ -41,10 +41,10 @@ def rules(tmp_path_factory):
     return ctypes.CDLL(str(d / "r.so"))
 
 
-def _plan(rules, hist, new, prefix, heads, mla, es=0):
+def _plan(rules, hist, new, prefix, heads, mla, es=0, max_q=None):
     ctx = [(m + n) >> es for m, n in zip(hist, new)]
-    args = (len(hist), sum(new), max(ctx), ctypes.c_long(sum(ctx)), prefix, heads, int(mla))
-    o = (ctypes.c_long * 11)()
+    args = (len(hist), sum(new), max_q or max(new), max(ctx), ctypes.c_long(sum(ctx)), prefix, heads, int(mla))
+    o = (ctypes.c_long * 12)()
     rules.plan(*args, o)
     p = dict(zip(NAMES, o))
     b = (ctypes.c_int * (4 * p["blocks"]))()
@@ -64,16 +64,21 @@ CASES = [
     ([700] * 300, [1] * 300, 640, 16, True),
     ([2000], [300], 0, 128, True),
     ([30000, 31000], [2000, 1500], 30000, 16, False),
+    ([900, 40, 2000, 900], [2, 0, 8, 1], 0, 16, True),
+    ([900, 940, 2000, 900], [8, 0, 8, 0], 900, 16, False),
+    ([5000] * 3, [1, 2, 1], 0, 64, True),
 ]
 
 
 @pytest.mark.parametrize("hist,new,prefix,heads,mla", CASES)
-def test_every_row_and_key_once(rules, hist, new, prefix, heads, mla):
-    p, blocks, ctx = _plan(rules, hist, new, prefix, heads, mla)
+@pytest.mark.parametrize("more", [0, 1000])  # a bound on the tokens of a session that is not tight
+def test_every_row_and_key_once(rules, hist, new, prefix, heads, mla, more):
+    p, blocks, ctx = _plan(rules, hist, new, prefix, heads, mla, max_q=max(new) + more)
+    assert p["one"] == (heads % 128 != 0 and (max(new) + more) * heads <= 128)
     q = np.concatenate([[0], np.cumsum(new)])
     rows = int(q[-1]) * heads
-    first = [rules.first(int(q[s]), heads, s) for s in range(len(hist))]
-    assert rules.first(int(q[-1]), heads, len(hist)) == p["own_tiles"]
+    first = [s if p["one"] else rules.first(int(q[s]), heads, s) for s in range(len(hist) + 1)]
+    assert first.pop() == p["own_tiles"]
     assert len(set(map(tuple, blocks))) == len(blocks) and p["chunk"] % 32 == 0
     seen = np.zeros(rows, np.int64)      # keys that blocks give the row
     slots = {}
@@ -116,5 +121,7 @@ def test_what_the_plan_aims_at(rules):
     p = _plan(rules, [16384] * 8, [213] * 8, 16384, 128, True)[0]
     assert p["whole"] == 8 * 213 // 256 * 256 and p["slots"] > 1
     assert _plan(rules, [16384] * 8, [32] * 8, 16384, 128, True)[0]["slots"] == 1
+    # no CU without a block because of tiles that may be empty
+    assert _plan(rules, [131072 + 1000] * 32, [1] * 32, 131072, 16, True)[0]["blocks"] == 256
     # one long row: many blocks
     assert _plan(rules, [131072], [1], 0, 128, True)[0]["blocks"] > 100
