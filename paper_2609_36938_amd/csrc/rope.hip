@@ -14,7 +14,7 @@
 // fp8 with one scale per token.  A token is LPR lanes (16, 64 or 256, by the
 // length of its row): an fp8 row's largest value is then a reduction over
 // those lanes, and short rows share a block.  A lane's unit is two groups of V
-// elements: the two halves of V pairs that lie apart, or 2 V neighbours.  Loads go out before the
+// elements, 16 bytes each (8 bf16, 4 fp32; 1 where an address or a size is odd).  Loads go out before the
 // angles are worked out.
 //
 // Bound by the bytes read and written where there are many (8192 tokens x 128 heads x 64 rotated
@@ -52,6 +52,8 @@ struct RopeArgs {
     int64_t o_rs, o_hs;          // bytes
     int plain_units;             // units a head of the elements that are only copied (0: in place)
     int turn_shift, plain_shift; // log2 of a head's units of both kinds, or -1
+    int pair_shift;              // log2 of a pair's elements that are neighbours
+    int plain_step, plain_gap;   // elements between units (log2), and between a unit's groups
     int scatter;                 // cache rows: to `rows`, or by context where it is null
     const int64_t *rows;
     int64_t num_rows;
@@ -133,18 +135,23 @@ JANUS_DEV void store_group(uint8_t *p, const float (&v)[V], float inv)
         if constexpr (V == 1) {
             *(float *)p = v[0];
         } else {
-            ((v4f *)p)[0] = v4f{v[0], v[1], v[2], v[3]};
-            ((v4f *)p)[1] = v4f{v[4], v[5], v[6], v[7]};
+#pragma unroll
+            for (int e = 0; e < V; e += 4)
+                *(v4f *)(p + 4 * e) = v4f{v[e], v[e + 1], v[e + 2], v[e + 3]};
         }
     } else if constexpr (DT == JANUS_BF16) {
         if constexpr (V == 1)
             *(uint16_t *)p = (uint16_t)bf16_pair(v[0], 0.f);
+        else if constexpr (V == 4)
+            *(v2i *)p = v2i{(int)bf16_pair(v[0], v[1]), (int)bf16_pair(v[2], v[3])};
         else
             *(v4i *)p = v4i{(int)bf16_pair(v[0], v[1]), (int)bf16_pair(v[2], v[3]), (int)bf16_pair(v[4], v[5]),
                             (int)bf16_pair(v[6], v[7])};
     } else {
         if constexpr (V == 1)
             *p = (uint8_t)fp8_quad(v[0] * inv, 0.f, 0.f, 0.f);
+        else if constexpr (V == 4)
+            *(uint32_t *)p = fp8_quad(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
         else
             *(v2i *)p = v2i{(int)fp8_quad(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv),
                             (int)fp8_quad(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv)};
@@ -152,7 +159,10 @@ JANUS_DEV void store_group(uint8_t *p, const float (&v)[V], float inv)
 }
 
 // Where a unit lies: its head, the first elements of its two groups in the
-// head (b < 0: one group), and its first pair (-1: not rotated).
+// head (b < 0: one group), and its first pair (-1: not rotated).  The groups are half of
+// the rotated, or of many plain, elements apart, so that neighbouring lanes' are neighbours
+// (8192 cache rows 6.9 us with groups side by side, 6.2 so; 1000 tokens x 128 heads x 128 fp32 in
+// interleaved pairs, with groups of eight, 30.5, and 21.5).
 struct Unit {
     int head, a, b, pair;
 };
@@ -165,16 +175,23 @@ JANUS_DEV Unit unit_at(const RopeArgs &g, int u)
     Unit at;
     if (u < first) {
         at.head = g.heads == 1 ? 0 : over(u, turned, g.turn_shift);
-        at.pair = (u - at.head * turned) * V;
-        at.a = g.off + (g.halves ? at.pair : 2 * at.pair);
-        at.b = at.a + (g.halves ? g.dim / 2 : V);
+        const int j = (u - at.head * turned) * V;
+        if constexpr (V > 1) {  // (a group of neighbours is whole pairs)
+            at.pair = j >> g.pair_shift;
+            at.a = g.off + j;
+            at.b = at.a + g.dim / 2;
+        } else {
+            at.pair = j;
+            at.a = g.off + (j << g.pair_shift);
+            at.b = at.a + (g.halves ? g.dim / 2 : 1);
+        }
     } else {
         u -= first;
         at.head = g.heads == 1 ? 0 : over(u, g.plain_units, g.plain_shift);
-        const int e = 2 * V * (u - at.head * g.plain_units);  // among the plain elements
+        const int e = (u - at.head * g.plain_units) << g.plain_step, f = e + g.plain_gap;  // among the plain elements
         at.pair = -1;
         at.a = e < g.off ? e : e + g.dim;
-        at.b = e + V < g.off ? e + V : e + V + g.dim;
+        at.b = f < g.off ? f : f + g.dim;
         if (at.b >= g.size)
             at.b = -1;
     }
@@ -267,7 +284,7 @@ __global__ __launch_bounds__(ROPE_THREADS) void rope_rows(RopeArgs g)
 #pragma unroll
                 for (int e = 0; e < V; e += 2) {
                     const float a = va[k][e], b = va[k][e + 1], c = vb[k][e], d = vb[k][e + 1];
-                    const float2 ta = t[e / 2], tb = t[(V + e) / 2];
+                    const float2 ta = t[e / 2], tb = t[g.dim / 4 + e / 2];
                     va[k][e] = a * ta.x - b * ta.y;
                     va[k][e + 1] = b * ta.x + a * ta.y;
                     vb[k][e] = c * tb.x - d * tb.y;
@@ -378,6 +395,11 @@ static void launch_rope_rows(RopeArgs g, hipStream_t st)
     const int turned = g.dim / (2 * V), units = g.heads * (turned + g.plain_units);
     g.turn_shift = pow2(turned) ? __builtin_ctz((unsigned)turned) : -1;
     g.plain_shift = pow2(g.plain_units) ? __builtin_ctz((unsigned)g.plain_units) : -1;
+    g.pair_shift = g.halves ? 0 : 1;
+    // Few plain elements of a head are one line of memory either way.
+    const bool many = g.plain_units >= 16;
+    g.plain_step = (V == 8 ? 3 : V == 4 ? 2 : 0) + !many;
+    g.plain_gap = many ? V * g.plain_units : V;
     auto go = [&](auto lanes, auto regs) {
         constexpr int LPR = decltype(lanes)::value, UPT = decltype(regs)::value;
         const int rows = ROPE_THREADS / LPR;
@@ -389,34 +411,36 @@ static void launch_rope_rows(RopeArgs g, hipStream_t st)
     // instructions whether or not it has a unit (8192 MLA rows, 36 units of 16 elements, 6.5 us
     // on 16 lanes of three units, 7.3 on 64 lanes of two).  Few rows: one unit a lane (64 of them 4.2 us, 4.6 with two).
     using std::integral_constant;
-    if (V > 1 && units <= 16)
-        go(integral_constant<int, 16>{}, integral_constant<int, 1>{});
-    else if (units <= 48 && (V == 1 || g.total_q >= 4096))
-        go(integral_constant<int, 16>{}, integral_constant<int, 3>{});
-    else if (V > 1 && units <= 64)
-        go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
-    else if (units <= 128)
-        go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+    constexpr int S = V == 4 ? 2 : 1;  // units of 16 elements in two
+    if (V > 1 && units <= 16 * S)
+        go(integral_constant<int, 16>{}, integral_constant<int, S>{});
+    else if (units <= 48 * S && (V == 1 || g.total_q >= 4096))
+        go(integral_constant<int, 16>{}, integral_constant<int, 3 * S>{});
+    else if (V > 1 && units <= 64 * S)
+        go(integral_constant<int, 64>{}, integral_constant<int, S>{});
+    else if (units <= 128 * S)
+        go(integral_constant<int, 64>{}, integral_constant<int, 2 * S>{});
     else
-        go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+        go(integral_constant<int, 256>{}, integral_constant<int, 2 * S>{});
 }
 
 template <class T>
 static int launch_rope(RopeArgs g, int x_dt, int out_dt, bool in_place, hipStream_t st)
 {
-    // Groups of eight where every one of them is 16 bytes (8 in fp8 rows) at an
-    // address of that alignment, else single elements.
+    // Groups of 16 bytes of x where every one of them lies at an address of that alignment
+    // (in fp8 rows 8), else single elements.
     const int64_t in = x_dt == JANUS_F32 ? 4 : 8, align = out_dt == JANUS_FP8_E4M3 ? 8 : 16;
     auto at = [](const void *p, int64_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; };
     const bool wide = g.dim % 16 == 0 && g.off % 8 == 0 && g.size % 8 == 0 && at(g.x, 16) && at(g.xr, 16) &&
                       at(g.out, align) && g.x_rs % in == 0 && g.x_hs % in == 0 && g.xr_rs % in == 0 &&
                       g.o_rs % align == 0 && g.o_hs % align == 0;
+    constexpr int V = 16 / sizeof(T);
     const int plain = in_place ? 0 : g.size - g.dim;
     auto go = [&](auto dt) {
         constexpr int DT = decltype(dt)::value;
         if (wide) {
-            g.plain_units = (plain + 15) / 16;
-            launch_rope_rows<T, DT, 8>(g, st);
+            g.plain_units = (plain + 2 * V - 1) / (2 * V);
+            launch_rope_rows<T, DT, V>(g, st);
         } else {
             g.plain_units = (plain + 1) / 2;
             launch_rope_rows<T, DT, 1>(g, st);
