@@ -514,7 +514,7 @@ JANUS_DEV void settled(v16f &s) { asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s));
 // 1.22 PFLOP/s on long ranges (8 sessions of 100 to 300 tokens x 128 heads on 17000 ids, 6.6 to
 // 6.9 ms), where a library product of 8192^3 reaches 1.22 and of 16384^3 1.40; they are busy in
 // 55% of the cycles.  Few rows pay 5 to 8 us before the first tile (queries and tiles from HBM), as
-// much behind the last, and the join: 32 sessions x 16 heads on 131072 ids take 170 us where
+// much behind the last, and the join: 32 sessions x 16 heads on 131072 ids take 163 us where
 // the product's rate would take 105.  The first form, with each wave's O^T rescaled
 // as maxima grow, spilled it and took 95 ms for the longest case; gathers left out behind the last
 // tile, by a branch, cost 7%.

@@ -18,9 +18,9 @@
 // angles are worked out.
 //
 // Bound by the bytes read and written where there are many (8192 tokens x 128 heads x 64 rotated
-// dims of bf16, 268 MB: 59 us, 4.5 TB/s; 2048 tokens x 64 heads x 128 dims to fp8, 50 MB: 11 us),
+// dims of bf16, 268 MB: 58 us, 4.6 TB/s; 2048 tokens x 64 heads x 128 dims to fp8, 50 MB: 11.4 us),
 // by one chain of loads (the session, its length, the frequencies' angles, the slot) where there are
-// few (16 decode queries 3.7 us, 64 cache rows to fp8 4.1; an empty kernel takes 2.5).  Loads behind
+// few (16 decode queries 3.6 us, 64 cache rows to fp8 4.1; an empty kernel takes 2.5).  Loads behind
 // branches, which wait for each other: 71 us for the first of these.
 #include "janus_device.hpp"
 #include "janus_host.hpp"
@@ -408,8 +408,8 @@ static void launch_rope_rows(RopeArgs g, hipStream_t st)
                            dim3(ROPE_THREADS), (size_t)rows * (g.dim / 2) * sizeof(float2), st, g);
     };
     // Many rows: the fewest lanes whose registers hold one, since a lane takes as many
-    // instructions whether or not it has a unit (8192 MLA rows, 36 units of 16 elements, 6.5 us
-    // on 16 lanes of three units, 7.3 on 64 lanes of two).  Few rows: one unit a lane (64 of them 4.2 us, 4.6 with two).
+    // instructions whether or not it has a unit (8192 MLA rows, 36 units of 16 elements, with
+    // groups side by side 6.5 us on 16 lanes of three units, 7.3 on 64 lanes of two).  Few rows: one unit a lane (64 of them 4.2 us, 4.6 with two).
     using std::integral_constant;
     constexpr int S = V == 4 ? 2 : 1;  // units of 16 elements in two
     if (V > 1 && units <= 16 * S)
