@@ -318,3 +318,19 @@ def test_replays_with_shorter_sessions(kind):
         torch.cuda.synchronize()
         c.hist = hist
         c.check(out, lse)
+
+
+def test_strides_of_their_own():
+    """K and V as halves of one row, and pools of different strides: what two plain pools give, bit by bit."""
+    c = Case([700, 705, 900], [1, 30, 2], 8, "mqa2", 699, 16)
+    want = c.run(out_dtype="f32")
+    n = c.k.shape[0]
+    both = torch.cat([c.k, c.v], 1).cuda()
+    k, v = torch.zeros((n, 136), dtype=torch.bfloat16), torch.zeros((n, 1024), dtype=torch.bfloat16)
+    k[:, :128], v[:, 512:640] = c.k, c.v
+    k, v = k.cuda(), v.cuda()
+    table = torch.from_numpy(c.table).cuda()
+    for kp, vp, ks, vs in ((both, both[:, 128:], 256, 256), (k, v[:, 512:], 136, 1024)):
+        got = janus.prefix_attn(c.bt, c.q.cuda(), kp, vp, table, 16, 699, float(c.scale), k_row_stride=ks, v_row_stride=vs,
+                                dv=128, out_dtype="f32", want_lse=True)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
