@@ -247,6 +247,7 @@ __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
     constexpr int GATHERS = KBUF / (1024 * PA_WAVES);    // a wave's, of each pool
     __shared__ __attribute__((aligned(16))) uint8_t ring[4 * BUF];
     __shared__ int sLim[PA_ROWS];
+    __shared__ __attribute__((aligned(16))) int sBad[PA_WAVES];  // a wave's `bad`
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c32 = lane & 31, hf = lane >> 5;
@@ -449,14 +450,22 @@ __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
         }
     }
 
-    __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
-    if (__syncthreads_or(bad)) {
+    const int mine = __ballot(bad) != 0;
+    if (lane == 0)
+        sBad[wave] = mine;
+    const float l = lsum + __shfl_xor(lsum, 32);
+    lds_barrier();
+    const v4i any = *(const v4i *)sBad;
+    if (__builtin_amdgcn_readfirstlane(any[0] | any[1] | any[2] | any[3])) {
+        __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
         plain_rows<128, 128>(g, r, sLim);
         return;
     }
-    const float l = lsum + __shfl_xor(lsum, 32);
-    if (!live)
+    // (the gathers behind the last tile still write LDS: a wave waits for its own before it ends)
+    if (!live) {
+        __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
         return;
+    }
     if (r.part >= 0) {
         const int64_t at = r.part + (row - r.row0);
         if (hf == 0)
@@ -469,6 +478,7 @@ __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
                     *(v4f *)(g.part + at * 128 + 32 * d + 2 * i + 4 * hf) =
                         v4f{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
         }
+        __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
         return;
     }
     const float inv = l != 0.f ? 1.f / l : 0.f;
@@ -480,6 +490,7 @@ __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
                        v4f{o[d][i] * inv, o[d][i + 1] * inv, o[d][i + 2] * inv, o[d][i + 3] * inv});
     if (g.lse && hf == 0)
         g.lse[row] = l != 0.f ? (m + log2f(l)) * LN2 : -INFINITY;
+    __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
 }
 
 constexpr int PM_KT = 32, PM_STEPS = 576 / 16;
