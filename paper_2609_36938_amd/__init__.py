@@ -110,6 +110,14 @@ def _ptr(t: Optional[torch.Tensor]):
     return ctypes.c_void_p(t.data_ptr())
 
 
+def _workspace(t: torch.Tensor, out: torch.Tensor):
+    """Address and bytes of a caller's workspace.  An empty tensor has no address, and NULL would be the size
+    query, which does nothing: it goes in as 0 bytes at out, which the library does not touch as a workspace."""
+    if not t.is_cuda:
+        raise JanusError("device tensor expected")
+    return t.data_ptr() or out.data_ptr(), ctypes.c_size_t(t.numel() * t.element_size())
+
+
 def _stream(stream=None):
     s = torch.cuda.current_stream() if stream is None else stream
     return ctypes.c_void_p(s.cuda_stream)
@@ -303,8 +311,8 @@ def sparse_attn_split(batch: Batch, q, k_pool, v_pool, page_table, page_size: in
     _check(lib().janus_sparse_attn_split(*args, None, ctypes.byref(need), _stream(stream)), "janus_sparse_attn_split")
     if workspace is None:
         workspace = torch.empty(max(int(need.value), 1), dtype=torch.uint8, device=q.device)
-    have = ctypes.c_size_t(workspace.numel() * workspace.element_size())
-    rc = lib().janus_sparse_attn_split(*args, _ptr(workspace), ctypes.byref(have), _stream(stream))
+    at, have = _workspace(workspace, out)
+    rc = lib().janus_sparse_attn_split(*args, at, ctypes.byref(have), _stream(stream))
     _check(rc, "janus_sparse_attn_split")
     return out, lse
 
@@ -354,8 +362,8 @@ def sparse_attn_fp8kv(batch: Batch, q, kv_pool, page_table, page_size: int, topk
     _check(lib().janus_sparse_attn_fp8kv(*args, None, ctypes.byref(need), _stream(stream)), "janus_sparse_attn_fp8kv")
     if workspace is None:
         workspace = torch.empty(max(int(need.value), 1), dtype=torch.uint8, device=q.device)
-    have = ctypes.c_size_t(workspace.numel() * workspace.element_size())
-    rc = lib().janus_sparse_attn_fp8kv(*args, _ptr(workspace), ctypes.byref(have), _stream(stream))
+    at, have = _workspace(workspace, out)
+    rc = lib().janus_sparse_attn_fp8kv(*args, at, ctypes.byref(have), _stream(stream))
     _check(rc, "janus_sparse_attn_fp8kv")
     return out, lse
 
@@ -637,11 +645,10 @@ def prefix_attn(batch: Batch, q, k_pool, v_pool, page_table, page_size: int, pre
     fn = lib().janus_prefix_attn
     args = (batch.ref, q.data_ptr(), Hq, dqk, dv, k_pool.data_ptr(), v_pool.data_ptr(), krs, vrs, page_table.data_ptr(),
             _table(batch, page_table, page_size), page_size, prefix_len, scale, out.data_ptr(), odt, _at(lse))
-    size = ctypes.c_size_t(0)
     if workspace is None:
-        _check(fn(*args, None, ctypes.byref(size), None), what)
-        workspace = _empty(torch.uint8, dev, stream, max(size.value, 1))
-    else:
-        size.value = workspace.numel() * workspace.element_size()
-    _launch(what, index, stream, fn, *args, workspace.data_ptr(), ctypes.byref(size))
+        need = ctypes.c_size_t(0)
+        _check(fn(*args, None, ctypes.byref(need), None), what)
+        workspace = _empty(torch.uint8, dev, stream, max(need.value, 1))
+    at, size = _workspace(workspace, out)
+    _launch(what, index, stream, fn, *args, at, ctypes.byref(size))
     return out, lse
