@@ -115,6 +115,8 @@ def _workspace(t: torch.Tensor, out: torch.Tensor):
     query, which does nothing: it goes in as 0 bytes at out, which the library does not touch as a workspace."""
     if not t.is_cuda:
         raise JanusError("device tensor expected")
+    if not t.is_contiguous():
+        raise JanusError("the workspace is to be contiguous: its bytes are counted by its elements")
     return t.data_ptr() or out.data_ptr(), ctypes.c_size_t(t.numel() * t.element_size())
 
 

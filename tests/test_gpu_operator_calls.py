@@ -60,3 +60,10 @@ def test_an_empty_workspace_of_the_split_attention(k, splits):
         else:
             with pytest.raises(janus.JanusError, match="workspace too small"):
                 call(out=out, workspace=_empty())
+
+
+def test_a_workspace_with_gaps():
+    """Every second byte of a buffer is no workspace, however many there are."""
+    args, dv = _prefix([9000], "mqa")
+    with pytest.raises(janus.JanusError, match="workspace"):
+        janus.prefix_attn(*args, dv=dv, workspace=torch.empty(64 << 20, dtype=torch.uint8, device="cuda")[::2])
