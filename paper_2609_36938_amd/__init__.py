@@ -613,20 +613,38 @@ def kv_append(batch: Batch, x, out, rotary: Optional[Rotary] = None, x_rot=None,
     return out
 
 
+def _row_stride(what: str, name: str, t, given: Optional[int]) -> int:
+    """Elements between the rows of a pool: as given, or those of the tensor, whose last dimension is a row and
+    whose other dimensions are the rows in order."""
+    if given is not None:
+        return int(given)
+    shape = t.shape
+    if len(shape) > 1:
+        if t.is_contiguous():
+            return shape[-1]
+        step = t.stride()
+        outer = [i for i in range(len(shape) - 1) if shape[i] > 1] or [len(shape) - 2]
+        if (step[-1] == 1 or shape[-1] == 1) and all(step[i] == step[j] * shape[j] for i, j in zip(outer, outer[1:])):
+            return step[outer[-1]]
+    raise JanusError(f"{what}: {name} is to be rows of adjacent elements at one distance from each other, not a "
+                     f"tensor of shape {tuple(shape)} and strides {t.stride()}")
+
+
 def prefix_attn(batch: Batch, q, k_pool, v_pool, page_table, page_size: int, prefix_len: int, scale: float,
                 k_row_stride: Optional[int] = None, v_row_stride: Optional[int] = None, dv: Optional[int] = None,
                 out_dtype: str = "bf16", want_lse: bool = False, out=None, lse=None, workspace=None, stream=None):
     """janus_prefix_attn: dense causal attention of the appended tokens over all
     cached ids, the first prefix_len of them common to the batch's sessions;
-    returns (out, lse or None).  q, pools, out and lse as for sparse_attn, workspace
-    as for sparse_attn_split."""
+    returns (out, lse or None).  q, out and lse as for sparse_attn, workspace as for
+    sparse_attn_split.  Pools are bf16 rows [..., elements], also views of wider ones, at
+    the tensors' own distances (or k_row_stride and v_row_stride elements apart)."""
     what = "janus_prefix_attn"
     total, shape, bf16, dev = batch.total_q, q.shape, torch.bfloat16, q.device
     if len(shape) != 3 or shape[0] != total or q.dtype is not bf16 or not q.is_contiguous():
         raise JanusError(f"{what}: q is to be a contiguous bfloat16 [{total}, heads, dims], not {tuple(shape)}")
     Hq, dqk = shape[1], shape[2]
-    krs = k_pool.shape[-1] if k_row_stride is None else int(k_row_stride)
-    vrs = v_pool.shape[-1] if v_row_stride is None else int(v_row_stride)
+    krs = _row_stride(what, "k_pool", k_pool, k_row_stride)
+    vrs = krs if v_pool is k_pool and v_row_stride is k_row_stride else _row_stride(what, "v_pool", v_pool, v_row_stride)
     if dv is None:
         dv = v_pool.shape[-1] if v_pool is not k_pool else dqk
     if k_pool.dtype is not bf16 or v_pool.dtype is not bf16 or out_dtype not in ("bf16", "f32"):

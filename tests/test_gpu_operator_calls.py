@@ -67,3 +67,40 @@ def test_a_workspace_with_gaps():
     args, dv = _prefix([9000], "mqa")
     with pytest.raises(janus.JanusError, match="workspace"):
         janus.prefix_attn(*args, dv=dv, workspace=torch.empty(64 << 20, dtype=torch.uint8, device="cuda")[::2])
+
+
+def test_pools_that_are_views():
+    """Rows of a wider cache, K and V as halves of a row, rows in pages: read where they lie."""
+    for kind, hist in (("mla", [100, 130]), ("mqa", [100, 130]), ("mla", [9000])):
+        args, dv = _prefix(hist, kind)
+        k, v = args[2], args[3]
+        want = janus.prefix_attn(*args, dv=dv, want_lse=True, out_dtype="f32")
+
+        def same(kp, vp, **kw):
+            got = janus.prefix_attn(*args[:2], kp, vp, *args[4:], want_lse=True, out_dtype="f32", **kw)
+            return all(torch.equal(a, b) for a, b in zip(got, want))
+
+        if kind == "mla":
+            wide = torch.full((len(k), 640), float("nan"), dtype=k.dtype, device="cuda")
+            wide[:, :576] = k
+            kv = wide[:, :576]
+            assert same(kv, kv, dv=dv)
+            assert same(kv, kv[:, :512])                         # V as the first elements of K's rows
+            assert same(kv.unflatten(0, (-1, 64)), kv.unflatten(0, (-1, 64))[..., :512])
+        else:
+            both = torch.cat([k, v], 1)
+            assert same(both[:, :128], both[:, 128:])
+            pages = both.view(-1, 64, 256)
+            assert same(pages[..., :128], pages[..., 128:])
+            assert same(both.view(-1, 64, 2, 128)[:, :, 0], both.view(-1, 64, 2, 128)[:, :, 1])
+            assert same(both, both[:, 128:], k_row_stride=256, v_row_stride=256, dv=128)
+
+
+def test_pools_whose_rows_have_no_one_distance():
+    args, dv = _prefix([100, 130], "mqa")
+    k, v = args[2], args[3]
+    gaps = torch.zeros((len(k) // 64, 65, 128), dtype=k.dtype, device="cuda")[:, :64]  # a row left out behind each page
+    flat = torch.zeros((128, len(k)), dtype=k.dtype, device="cuda").T                 # elements apart
+    for kp, vp in ((gaps, v), (k, gaps), (flat, v), (k, flat), (k.view(-1), v), (k, v.view(-1))):
+        with pytest.raises(janus.JanusError, match="pool"):
+            janus.prefix_attn(*args[:2], kp, vp, *args[4:], dv=dv)
