@@ -649,6 +649,8 @@ def prefix_attn(batch: Batch, q, k_pool, v_pool, page_table, page_size: int, pre
         dv = v_pool.shape[-1] if v_pool is not k_pool else dqk
     if k_pool.dtype is not bf16 or v_pool.dtype is not bf16 or out_dtype not in ("bf16", "f32"):
         raise JanusError(f"{what}: bfloat16 pools and out_dtype bf16 or f32 expected")
+    if not 0 <= prefix_len <= batch.max_ctx:  # (past 32 bits it would wrap round on its way)
+        raise JanusError(f"{what}: prefix_len is to be 0 to {batch.max_ctx}, not {prefix_len}")
     _want(what, "page_table", page_table, torch.int32, batch.c.num_seqs, None)
     odt, torch_dt = (JANUS_BF16, bf16) if out_dtype == "bf16" else (JANUS_F32, torch.float32)
     if out is None:

@@ -104,3 +104,10 @@ def test_pools_whose_rows_have_no_one_distance():
     for kp, vp in ((gaps, v), (k, gaps), (flat, v), (k, flat), (k.view(-1), v), (k, v.view(-1))):
         with pytest.raises(janus.JanusError, match="pool"):
             janus.prefix_attn(*args[:2], kp, vp, *args[4:], dv=dv)
+
+
+def test_a_prefix_beyond_32_bits_is_refused():
+    args, dv = _prefix([100], "mqa")
+    for n in (-1, 102, (1 << 32) + 64):
+        with pytest.raises(janus.JanusError):
+            janus.prefix_attn(*args[:6], n, args[7], dv=dv)
