@@ -399,6 +399,15 @@ def _at(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
+def _no_gradient(what: str, *tensors):
+    """The calls record nothing for autograd: a tensor that it follows is refused rather than cut off from it."""
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise JanusError(f"{what}: a gradient would be lost here; call under torch.no_grad(), or in the forward "
+                                 "and backward functions of a torch.autograd.Function")
+
+
 def _empty(dtype, device, stream, *shape):
     """A new tensor that belongs to the stream of the launch: its memory is not given to other
     streams' work before, or after it is dropped, while that launch may use it.  (torch takes sizes
@@ -534,7 +543,8 @@ def rope(batch: Batch, rotary: Rotary, x, out=None, out_dtype: Optional[str] = N
 
     out: a tensor of x's shape, x itself to turn it in place, or None for a new
     one; out_dtype "f32", "bf16" or "fp8" (None: out's, or x's).  fp8 outputs are e4m3
-    bytes (uint8, or float8_e4m3fn if given) with one scale per token."""
+    bytes (uint8, or float8_e4m3fn if given) with one scale per token.  Nothing is recorded
+    for autograd: the gradient of x is rope of out's gradient with rotary.inverted()."""
     what = "janus_rope"
     total, shape = batch.total_q, x.shape
     if len(shape) != 3 or shape[0] != total:
@@ -562,6 +572,7 @@ def rope(batch: Batch, rotary: Rotary, x, out=None, out_dtype: Optional[str] = N
         raise JanusError(f"{what}: out_scale goes with fp8 outputs")
     if rotary.positions is not None:
         rotary._check(what, batch)
+    _no_gradient(what, x, out, out_scale)
     dev = _device(what, x, out, out_scale, batch.q_start, rotary.inv_freq)
     if total:
         _launch(what, dev, stream, lib().janus_rope, batch.ref, rotary.ref, x.data_ptr(), xdt, xs[0], xs[1], shape[1],
@@ -605,6 +616,7 @@ def kv_append(batch: Batch, x, out, rotary: Optional[Rotary] = None, x_rot=None,
             raise JanusError(f"{what}: out_scale is to hold one float32 for each of {num_rows} rows")
     if rotary is not None and rotary.positions is not None:
         rotary._check(what, batch)
+    _no_gradient(what, x, x_rot, out, out_scale)
     dev = _device(what, out, x, x_rot, rows, out_scale, batch.q_start, None if rotary is None else rotary.inv_freq)
     if total:
         _launch(what, dev, stream, lib().janus_kv_append, batch.ref, None if rotary is None else rotary.ref, _at(x),
@@ -661,6 +673,7 @@ def prefix_attn(batch: Batch, q, k_pool, v_pool, page_table, page_size: int, pre
         _want(what, "lse", lse, torch.float32, total, Hq)
     elif want_lse:
         lse = _empty(torch.float32, dev, stream, total, Hq)
+    _no_gradient(what, q, k_pool, v_pool, out, lse)
     index = _device(what, q, k_pool, v_pool, page_table, out, lse, workspace, batch.q_start)
     if total == 0:
         return out, lse

@@ -111,3 +111,41 @@ def test_a_prefix_beyond_32_bits_is_refused():
     for n in (-1, 102, (1 << 32) + 64):
         with pytest.raises(janus.JanusError):
             janus.prefix_attn(*args[:6], n, args[7], dv=dv)
+
+
+def test_tensors_that_autograd_follows():
+    """The calls record no gradient: they refuse to lose one, and run where none is asked for."""
+    bt, rot = janus.Batch([5], [3]), janus.Rotary(64)
+    x = _randn((3, 2, 64), 1, torch.float32).requires_grad_()
+    pool = torch.zeros((64, 64), device="cuda")
+    args, dv = _prefix([100], "mqa")
+    calls = [lambda: janus.rope(bt, rot, x), lambda: janus.rope(bt, rot, x.detach(), out=torch.zeros_like(x) * x),
+             lambda: janus.kv_append(bt, x[:, 0], pool, rot), lambda: janus.kv_append(bt, None, pool, rot, x[:, 0]),
+             lambda: janus.kv_append(bt, x[:, 0].detach(), pool.clone().requires_grad_(), rot)]
+    for i in (1, 2, 3):
+        leaf = args[i].clone().requires_grad_()
+        calls.append(lambda i=i, leaf=leaf: janus.prefix_attn(*args[:i], leaf, *args[i + 1:], dv=dv))
+    for call in calls:
+        with pytest.raises(janus.JanusError, match="gradient"):
+            call()
+        with torch.no_grad():
+            call()
+
+
+def test_a_function_with_the_transpose_as_its_backward():
+    """What a caller wraps the two calls in: its gradient is the transpose, and gradcheck's differences agree."""
+    bt, rot = janus.Batch([70], [3]), janus.Rotary(32, 8)
+
+    class Turn(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x):
+            return janus.rope(bt, rot, x)[0]
+
+        @staticmethod
+        def backward(ctx, g):
+            return janus.rope(bt, rot.inverted(), g.contiguous())[0]
+
+    x = _randn((3, 2, 64), 1, torch.float32).requires_grad_()
+    w = _randn((3, 2, 64), 2, torch.float32)
+    (Turn.apply(x) * w).sum().backward()
+    assert torch.equal(x.grad, janus.rope(bt, rot.inverted(), w)[0])
