@@ -408,6 +408,11 @@ def _no_gradient(what: str, *tensors):
                                  "and backward functions of a torch.autograd.Function")
 
 
+def _written(*tensors):
+    """Tensors of the caller's that a call has written: a graph that keeps one for its backward pass will notice."""
+    torch.autograd.graph.increment_version([t for t in tensors if t is not None])
+
+
 def _empty(dtype, device, stream, *shape):
     """A new tensor that belongs to the stream of the launch: its memory is not given to other
     streams' work before, or after it is dropped, while that launch may use it.  (torch takes sizes
@@ -520,6 +525,7 @@ def page_grow(batch: Batch, page_size: int, free_list, page_table, free_head=Non
     _launch(what, dev, stream, lib().janus_page_grow, batch.ref, page_size, free_list.data_ptr(), free_list.numel(),
             _at(free_head), page_table.data_ptr(), _table(batch, page_table, page_size),
             slots.data_ptr() if total else at, at)
+    _written(page_table, slots, counts)
     return page_table, slots, counts
 
 
@@ -577,6 +583,7 @@ def rope(batch: Batch, rotary: Rotary, x, out=None, out_dtype: Optional[str] = N
     if total:
         _launch(what, dev, stream, lib().janus_rope, batch.ref, rotary.ref, x.data_ptr(), xdt, xs[0], xs[1], shape[1],
                 shape[2], out.data_ptr(), odt, os_[0], os_[1], _at(out_scale))
+        _written(out, out_scale)
     return out, out_scale
 
 
@@ -622,6 +629,7 @@ def kv_append(batch: Batch, x, out, rotary: Optional[Rotary] = None, x_rot=None,
         _launch(what, dev, stream, lib().janus_kv_append, batch.ref, None if rotary is None else rotary.ref, _at(x),
                 xdt, 0 if x is None else x.stride(0), _at(x_rot), 0 if x_rot is None else x_rot.stride(0), n,
                 _at(rows), num_rows, out.data_ptr(), odt, width * out.element_size(), _at(out_scale))
+        _written(out, out_scale)
     return out
 
 
@@ -686,4 +694,5 @@ def prefix_attn(batch: Batch, q, k_pool, v_pool, page_table, page_size: int, pre
         workspace = _empty(torch.uint8, dev, stream, max(need.value, 1))
     at, size = _workspace(workspace, out)
     _launch(what, index, stream, fn, *args, at, ctypes.byref(size))
+    _written(out, lse)
     return out, lse

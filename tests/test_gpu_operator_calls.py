@@ -149,3 +149,32 @@ def test_a_function_with_the_transpose_as_its_backward():
     w = _randn((3, 2, 64), 2, torch.float32)
     (Turn.apply(x) * w).sum().backward()
     assert torch.equal(x.grad, janus.rope(bt, rot.inverted(), w)[0])
+
+
+def test_what_a_call_writes_counts_as_changed():
+    """A tensor that a graph keeps for its backward pass and a call then writes: the pass says so."""
+    bt, rot = janus.Batch([5], [3]), janus.Rotary(64)
+    args, dv = _prefix([100], "mqa")
+    out = torch.zeros((1, 16, 128), dtype=torch.bfloat16, device="cuda")
+    lse = torch.zeros((1, 16), device="cuda")
+    x = _randn((3, 2, 64), 1, torch.float32)
+    pool, scale = torch.zeros((64, 64), device="cuda"), torch.zeros(3, device="cuda")
+    codes, row_scale = torch.zeros((64, 64), dtype=torch.uint8, device="cuda"), torch.zeros(64, device="cuda")
+    fp8 = torch.zeros((3, 2, 64), dtype=torch.uint8, device="cuda")
+    table = torch.zeros((1, 1), dtype=torch.int32, device="cuda")
+    free = torch.arange(8, dtype=torch.int32, device="cuda")
+    given = torch.zeros(3, dtype=torch.int64, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+    for call, written in ((lambda: janus.rope(bt, rot, x, out=x), [x]),
+                          (lambda: janus.rope(bt, rot, x, out=fp8, out_scale=scale), [fp8, scale]),
+                          (lambda: janus.kv_append(bt, x[:, 0], pool, rot), [pool]),
+                          (lambda: janus.kv_append(bt, x[:, 0], codes, rot, out_scale=row_scale), [codes, row_scale]),
+                          (lambda: janus.page_grow(bt, 64, free, table, out=given), [table, *given]),
+                          (lambda: janus.prefix_attn(*args, dv=dv, out=out, lse=lse), [out, lse])):
+        before = [t._version for t in written]
+        call()
+        assert all(t._version > v for t, v in zip(written, before))
+    w = torch.ones((3, 2, 64), device="cuda", requires_grad=True)
+    y = (w * x).sum()
+    janus.rope(bt, rot, x, out=x)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
