@@ -469,8 +469,8 @@ int janus_rotary_frequencies(int dim, double base, double factor, int scaling, i
  *   out_scale  device [total_q] fp32 for fp8, NULL otherwise
  * fp8 outputs are quantised over all heads of a token, as janus_index_scores
  * takes its queries: out_scale = max(largest finite magnitude, 1e-12) / 448 and
- * out = the nearest e4m3 of value / out_scale (infinities as the largest value, NaN as
- * NaN).  Angles are reduced in fp64, the rotation is fp32, and results are
+ * out = value / out_scale, rounded to fp32 and then to e4m3, both to nearest (infinities
+ * as the largest value, NaN as NaN).  Angles are reduced in fp64, the rotation is fp32, and results are
  * rounded to out_dt once.  Rows from q_start[B] on are left as they are.
  * heads * size up to 2^24 and fewer than 2^24 tokens (else JANUS_ERR_UNSUPPORTED).
  */

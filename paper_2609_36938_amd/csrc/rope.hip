@@ -128,8 +128,21 @@ JANUS_DEV uint32_t fp8_quad(float a, float b, float c, float d)
     return __builtin_bit_cast(uint32_t, w);
 }
 
+// An fp8 row's scale, and its reciprocal rounded to nearest.
+struct Scale {
+    float step, inv;
+    // v / step rounded to nearest: the product with the reciprocal, corrected once by its remainder, which
+    // an fma gives exactly (Markstein, IBM J. Res. Dev. 34, 1990).  The product alone is off by up to an ulp and
+    // a half, which takes values next to a border of e4m3 to its other side.  (A zero keeps its sign.)
+    JANUS_DEV float of(float v) const
+    {
+        const float q = v * inv;
+        return copysignf(fmaf(fmaf(-q, step, v), inv, q), v);
+    }
+};
+
 template <int DT, int V>
-JANUS_DEV void store_group(uint8_t *p, const float (&v)[V], float inv)
+JANUS_DEV void store_group(uint8_t *p, const float (&v)[V], Scale s)
 {
     if constexpr (DT == JANUS_F32) {
         if constexpr (V == 1) {
@@ -149,12 +162,12 @@ JANUS_DEV void store_group(uint8_t *p, const float (&v)[V], float inv)
                             (int)bf16_pair(v[6], v[7])};
     } else {
         if constexpr (V == 1)
-            *p = (uint8_t)fp8_quad(v[0] * inv, 0.f, 0.f, 0.f);
+            *p = (uint8_t)fp8_quad(s.of(v[0]), 0.f, 0.f, 0.f);
         else if constexpr (V == 4)
-            *(uint32_t *)p = fp8_quad(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+            *(uint32_t *)p = fp8_quad(s.of(v[0]), s.of(v[1]), s.of(v[2]), s.of(v[3]));
         else
-            *(v2i *)p = v2i{(int)fp8_quad(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv),
-                            (int)fp8_quad(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv)};
+            *(v2i *)p = v2i{(int)fp8_quad(s.of(v[0]), s.of(v[1]), s.of(v[2]), s.of(v[3])),
+                            (int)fp8_quad(s.of(v[4]), s.of(v[5]), s.of(v[6]), s.of(v[7]))};
     }
 }
 
@@ -294,20 +307,20 @@ __global__ __launch_bounds__(ROPE_THREADS) void rope_rows(RopeArgs g)
         }
     };
     constexpr int BYTES = FP8 ? 1 : DT == JANUS_BF16 ? 2 : 4;
-    auto put = [&](int first, float inv) {
+    auto put = [&](int first, Scale scale) {
 #pragma unroll
         for (int k = 0; k < UPT; ++k) {
             if (first + k * LPR + lane >= units || !store)
                 continue;
             uint8_t *p = g.out + to * g.o_rs + (int64_t)at[k].head * g.o_hs;
-            store_group<DT, V>(p + (int64_t)at[k].a * BYTES, va[k], inv);
+            store_group<DT, V>(p + (int64_t)at[k].a * BYTES, va[k], scale);
             if (at[k].b >= 0)
-                store_group<DT, V>(p + (int64_t)at[k].b * BYTES, vb[k], inv);
+                store_group<DT, V>(p + (int64_t)at[k].b * BYTES, vb[k], scale);
         }
     };
     rotate();
     if constexpr (!FP8) {
-        put(u0, 1.f);
+        put(u0, Scale{1.f, 1.f});
     } else {
         // Largest magnitude of the token (fmaxf passes over NaN), and if that is
         // infinite, the largest finite one: infinities are then written as the largest e4m3.
@@ -367,7 +380,8 @@ __global__ __launch_bounds__(ROPE_THREADS) void rope_rows(RopeArgs g)
             if (!again)
                 fit();
         }
-        const float scale = fmaxf(top, AMAX_FLOOR) / FP8_LARGEST, inv = 1.f / scale;
+        const float step = fmaxf(top, AMAX_FLOOR) / FP8_LARGEST;
+        const Scale scale = {step, 1.f / step};
         if (again) {
             // a row longer than the lanes' registers is read again
             for (int u = 0; u < units; u += LPR * UPT) {
@@ -375,16 +389,16 @@ __global__ __launch_bounds__(ROPE_THREADS) void rope_rows(RopeArgs g)
                 rotate();
                 if (odd)
                     fit();
-                put(u, inv);
+                put(u, scale);
             }
         } else {
-            put(0, inv);
+            put(0, scale);
         }
         if (lane == 0 && store) {
             if (g.scale)
-                g.scale[to] = scale;
+                g.scale[to] = step;
             else
-                *(float *)(g.out + to * g.o_rs + g.size) = scale;
+                *(float *)(g.out + to * g.o_rs + g.size) = step;
         }
     }
 }

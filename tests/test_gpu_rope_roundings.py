@@ -1,0 +1,50 @@
+"""The roundings of janus_rope and janus_kv_append."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+janus = pytest.importorskip("paper_2609_36938_amd")
+
+
+def _near_borders(rows, n, seed):
+    """fp32 rows whose quotients by the row's scale lie at and next to the borders between two e4m3 values."""
+    rng = np.random.default_rng(seed)
+    codes = np.arange(0x7e, dtype=np.uint8)            # 0 .. 416, and 448 above the last
+    held = torch.from_numpy(np.append(codes, 0x7e).astype(np.uint8)).view(torch.float8_e4m3fn).double().numpy()
+    border = (held[:-1] + held[1:]) / 2
+    x = np.empty((rows, n), np.float32)
+    for r in range(rows):
+        top = np.float32(np.exp(rng.uniform(-20, 20)))
+        scale = np.float32(top / np.float32(448))
+        at = (border[rng.integers(0, len(border), n)] * np.float64(scale)).astype(np.float32)
+        for _ in range(2):
+            up = rng.random(n) < 0.3
+            at[up] = np.nextafter(at[up], np.float32(np.inf))
+            down = rng.random(n) < 0.3
+            at[down] = np.nextafter(at[down], np.float32(0))
+        x[r] = np.where(rng.random(n) < 0.5, at, -at)
+        x[r, n - 1 - rng.integers(0, n // 2)] = top
+    return torch.from_numpy(x)
+
+
+def _codes(x, scale):
+    """e4m3 of the fp32 quotients, both rounded to nearest (on the CPU)."""
+    return (x / scale[:, None]).to(torch.float8_e4m3fn).view(torch.uint8)
+
+
+@pytest.mark.parametrize("size,dim,T", [(128, 16, 600), (576, 64, 5000), (130, 2, 600), (9000, 16, 20)])
+def test_fp8_next_to_a_border(size, dim, T):
+    """Elements that are only copied: their codes are exact, in queries and in cache rows."""
+    x = _near_borders(T, size, size)
+    x[:, :dim] = 0
+    bt, rot = janus.Batch([0], [T]), janus.Rotary(dim)
+    want_scale = x.abs().amax(1) / torch.tensor(448.0)
+    want = _codes(x, want_scale)[:, dim:]
+    out, scale = janus.rope(bt, rot, x[:, None].cuda(), out_dtype="fp8")
+    assert torch.equal(scale.cpu(), want_scale)
+    assert torch.equal(out[:, 0, dim:].cpu(), want)
+    pool = torch.zeros((T, size), dtype=torch.uint8, device="cuda")
+    scales = torch.zeros(T, device="cuda")
+    janus.kv_append(bt, x.cuda(), pool, rot, rows=torch.arange(T, device="cuda"), out_scale=scales)
+    assert torch.equal(scales.cpu(), want_scale) and torch.equal(pool[:, dim:].cpu(), want)
