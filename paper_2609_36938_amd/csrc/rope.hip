@@ -5,9 +5,11 @@
 //   (m (x_a cos t - x_b sin t), m (x_b cos t + x_a sin t)),  t = position * inv_freq[pair]
 //
 // (t negated for the transpose).  t is reduced to a fraction of a turn in 64
-// bits, where far positions lose nothing, and its sine and cosine are taken of
-// that fraction in 32.  They are worked out once per token and pair, into LDS,
-// and used by all heads.
+// bits, where far positions lose nothing.  Sine and cosine are taken of that fraction
+// rounded to 32, and turned on by the angle d that the rounding lost (under 1e-7, so
+// sin(a + d) = sin a + d cos a and cos(a + d) = cos a - d sin a to fp32's last bit):
+// without that a sine near 0 keeps none of its bits.  They are worked out once per
+// token and pair, into LDS, and used by all heads.
 //
 // One kernel does queries (many heads a token, written in place or apart) and
 // cache rows (one head a token, scattered through a slot map), to fp32, bf16 or
@@ -268,8 +270,10 @@ __global__ __launch_bounds__(ROPE_THREADS) void rope_rows(RopeArgs g)
     for (int p = lane; p < pairs; p += LPR) {
         double t = (double)pos * (p < LPR ? freq : g.inv_freq[p]) * 0.15915494309189533577;  // turns
         t -= rint(t);
-        float s, c;
-        sincospif(2.f * (float)t, &s, &c);
+        const float hi = (float)t, lo = (float)(t - (double)hi) * 6.2831853071795865f;
+        float s0, c0;
+        sincospif(2.f * hi, &s0, &c0);
+        const float s = fmaf(lo, c0, s0), c = fmaf(-lo, s0, c0);
         turn[mine * pairs + p] = float2{c * g.mag, (g.inverse ? -s : s) * g.mag};
     }
     if constexpr (LPR > kWave)

@@ -48,3 +48,28 @@ def test_fp8_next_to_a_border(size, dim, T):
     scales = torch.zeros(T, device="cuda")
     janus.kv_append(bt, x.cuda(), pool, rot, rows=torch.arange(T, device="cuda"), out_scale=scales)
     assert torch.equal(scales.cpu(), want_scale) and torch.equal(pool[:, dim:].cpu(), want)
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("pairs", [64, 20])
+def test_sines_next_to_their_zeros(layout, pairs):
+    """(1, 0) turned is (cos t, sin t).  The angle is reduced in 64 bits and its rounding to 32 made good, so each is
+    within 2^-21 of its own size: the library's sine and cosine of the rounded fraction of a turn (2 ulp, 2^-22, of results
+    that are at least half as large as the one sought or replaced by the correction), the correction and its sum 2^-23.
+    What 64 bits lose, here and in the kernel, is 4 * 2^-53 of the angle.  (A fraction of a turn that is
+    rounded to 32 bits alone would be off by 2^-26 turns, 9e-8, however small the sine.)"""
+    T = 20000
+    rng = np.random.default_rng(pairs)
+    freq = np.exp(rng.uniform(-7, 0, pairs))
+    pos = rng.integers(0, 1 << 17, T).astype(np.int32)
+    rot = janus.Rotary(2 * pairs, layout=layout, inv_freq=torch.from_numpy(freq).cuda(), positions=torch.from_numpy(pos).cuda())
+    x = torch.zeros((T, 1, 2 * pairs), device="cuda")
+    first = slice(0, pairs) if layout == "half" else slice(0, None, 2)
+    second = slice(pairs, None) if layout == "half" else slice(1, None, 2)
+    x[..., first] = 1
+    y = janus.rope(janus.Batch([0], [T]), rot, x)[0][:, 0].double().cpu().numpy()
+    t = pos[:, None] * freq
+    for got, want in ((y[:, first], np.cos(t)), (y[:, second], np.sin(t))):
+        assert np.abs(want).min() < 2e-5
+        tol = 2.0 ** -21 * np.abs(want) + 4 * 2.0 ** -53 * np.abs(t)
+        assert (np.abs(got - want) <= tol).all(), (np.abs(got - want) / np.abs(want)).max()
