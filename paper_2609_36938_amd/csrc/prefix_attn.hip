@@ -155,6 +155,25 @@ JANUS_DEV int block_limit(const PrefixRange &r, const int *lim)
     return __builtin_amdgcn_readfirstlane(least);
 }
 
+// A row's sum of probabilities, over a range of any length: a tile's are added pairwise, and the
+// tiles' sums with what each addition rounds off carried to the next (Kahan, CACM 8, 1965).  One
+// after the other in fp32, half a million equal terms are off by 2e-3.
+struct Total {
+    float sum, off;
+    JANUS_DEV void add(float x)
+    {
+        const float y = x - off, t = sum + y;
+        off = (t - sum) - y;
+        sum = t;
+    }
+    JANUS_DEV void scale(float f)
+    {
+        sum *= f;
+        off *= f;
+    }
+};
+JANUS_DEV float sum8(v8f p) { return ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7])); }
+
 // The block's rows without matrix instructions: a wave a row, a lane a key, then DV / 64 dims.
 // For blocks that hold an infinity or NaN in a row of V of a tile in which rows end
 // at different keys: a probability of 0 does not undo it for the rows without the key.
@@ -170,7 +189,8 @@ JANUS_DEV void plain_rows(const PrefixArgs &g, const PrefixRange &r, const int *
     for (int row = r.row0 + (threadIdx.x >> 6); row < r.row1; row += PA_WAVES) {
         const uint16_t *q = g.q + (int64_t)row * DQK;
         const int end = lim[row - r.row0];
-        float m = M_INIT, l = 0.f, acc[N] = {};
+        float m = M_INIT, acc[N] = {};
+        Total sum = {0.f, 0.f};
         for (int k0 = r.kbeg; k0 < end; k0 += 64) {
             float x = -INFINITY;
             if (k0 + lane < end) {
@@ -187,20 +207,25 @@ JANUS_DEV void plain_rows(const PrefixArgs &g, const PrefixRange &r, const int *
             const float mnew = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f(m - mnew);
             m = mnew;
             const float p = k0 + lane < end ? __builtin_amdgcn_exp2f(x - m) : 0.f;
-            l *= alpha;
+            sum.scale(alpha);
+            float tile = p;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1)
+                tile += __shfl_xor(tile, o);
+            sum.add(tile);
 #pragma unroll
             for (int e = 0; e < N; ++e)
                 acc[e] *= alpha;
             for (int j = 0; j < min(64, end - k0); ++j) {
                 const float pj = __shfl(p, j);
                 const uint16_t *v = (const uint16_t *)(g.v + slot(k0 + j) * g.v_rb) + N * lane;
-                l += pj;
 #pragma unroll
                 for (int e = 0; e < N; ++e)
                     acc[e] = fmaf(pj, bf16_to_f32(v[e]), acc[e]);
             }
         }
         const int64_t at = r.part + (row - r.row0);
+        const float l = sum.sum;
         const float inv = l != 0.f ? 1.f / l : 0.f;
 #pragma unroll
         for (int e = 0; e < N; ++e) {
@@ -275,7 +300,8 @@ __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
 #pragma unroll
         for (int i = 0; i < 16; ++i)
             o[d][i] = 0.f;
-    float m = M_INIT, lsum = 0.f;
+    float m = M_INIT;
+    Total lsum = {0.f, 0.f};
     int bad = 0;   // a tile where rows end holds values of V that are not finite
     int bmin = 0;  // keys before it are every row's
 
@@ -381,7 +407,7 @@ __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
             mx = fmaxf(mx, __shfl_xor(mx, 32));
             const float mnew = mx > m + RESCALE_SLACK ? mx : m;
             const float alpha = __builtin_amdgcn_exp2f(m - mnew);
-            lsum *= alpha;
+            lsum.scale(alpha);
             m = mnew;
 #pragma unroll
             for (int d = 0; d < NB; ++d)
@@ -391,16 +417,17 @@ __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
         }
         ahead = logits(ring + (SLOT + 1) % 4 * BUF);
         v8bf pb[2];
+        float sums[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             v8f p;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
+            for (int e = 0; e < 8; ++e)
                 p[e] = __builtin_amdgcn_exp2f(s[8 * h + e] * mult - m);
-                lsum += p[e];
-            }
+            sums[h] = sum8(p);
             pb[h] = __builtin_convertvector(p, v8bf);
         }
+        lsum.add(sums[0] + sums[1]);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -453,7 +480,7 @@ __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
     const int mine = __ballot(bad) != 0;
     if (lane == 0)
         sBad[wave] = mine;
-    const float l = lsum + __shfl_xor(lsum, 32);
+    const float l = lsum.sum + __shfl_xor(lsum.sum, 32);
     lds_barrier();
     const v4i any = *(const v4i *)sBad;
     if (__builtin_amdgcn_readfirstlane(any[0] | any[1] | any[2] | any[3])) {
@@ -564,7 +591,8 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
     }
     // O^T of dims 128 wave + 32 d .. and rows 32 rb ..
     v16f o[4][PA_WAVES];
-    float m = M_INIT, lsum = 0.f;
+    float m = M_INIT;
+    Total lsum = {0.f, 0.f};
 
     const int base0 = kbeg & ~(PM_KT - 1);
     const int nt = kend > kbeg ? (kend - base0 + PM_KT - 1) / PM_KT : 0;
@@ -733,16 +761,17 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
             over |= m != M_INIT && mx > m + PM_HEADROOM;
             m = m == M_INIT ? fmaxf(mx, M_INIT) : m;
         }
+        float sums[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             v8f p;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
+            for (int e = 0; e < 8; ++e)
                 p[e] = __builtin_amdgcn_exp2f(s[8 * h + e] * mult - m);
-                lsum += p[e];
-            }
+            sums[h] = sum8(p);
             pb[h] = __builtin_convertvector(p, v8bf);
         }
+        lsum.add(sums[0] + sums[1]);
     };
     auto give = [&](int t) {
         sP[t & 1][wave][0][lane] = __builtin_bit_cast(v4i, pb[0]);
@@ -761,7 +790,7 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
 #pragma unroll
                     for (int i = 0; i < 16; ++i)
                         o[d][rb][i] = 0.f;
-            lsum = 0.f;
+            lsum = {0.f, 0.f};
             logits(0, std::integral_constant<int, 0>{}, 0);
             probabilities(mask(0));
             give(0);
@@ -837,7 +866,7 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
         plain_rows<576, 512>(g, r, sLim);
         return;
     }
-    const float l = lsum + __shfl_xor(lsum, 32);
+    const float l = lsum.sum + __shfl_xor(lsum.sum, 32);
     if (hf == 0) {
         sM[32 * wave + c32] = m;
         sL[32 * wave + c32] = l;

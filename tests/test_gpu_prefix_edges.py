@@ -1,0 +1,40 @@
+"""janus_prefix_attn at its edges."""
+import numpy as np
+import pytest
+import torch
+
+from test_prefix_plan import _plan, rules  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+janus = pytest.importorskip("paper_2609_36938_amd")
+
+
+@pytest.mark.parametrize("kind,heads,hist,new", [("mqa2", 16, 524288 - 8192, 8192), ("mla", 128, 524288 - 512, 512)])
+def test_the_sum_over_many_keys(rules, kind, heads, hist, new):  # noqa: F811
+    """Keys that all score alike, below the first: a range of 500000 of them in one block.  Logits are exact (one
+    product of powers of two), so the sum is off by its own roundings alone.  The pool is two pages."""
+    dqk, dv = (576, 512) if kind == "mla" else (128, 128)
+    p = _plan(rules, [hist], [new], 0, heads, kind == "mla")[0]
+    assert p["whole"] == p["own_tiles"] and p["slots"] == 1
+    scale, low = 2.0 ** -4, 11.0                       # logits 16 and 11, in 2^-4 * 16 * 16 and 2^-4 * 16 * 11
+    k = torch.zeros((128, dqk), dtype=torch.bfloat16)
+    k[:, 0] = low
+    k[0, 0] = 16
+    k[:, 1] = 0.75                                     # (a value, q has 0 there)
+    v = k if kind == "mla" else torch.full((128, dv), 0.75, dtype=torch.bfloat16)
+    q = torch.zeros((new, heads, dqk), dtype=torch.bfloat16)
+    q[..., 0] = 16
+    table = torch.ones((1, (hist + new) // 64), dtype=torch.int32)
+    table[0, 0] = 0
+    kd, vd = k.cuda(), None
+    vd = kd if kind == "mla" else v.cuda()
+    out, lse = janus.prefix_attn(janus.Batch([hist], [new]), q.cuda(), kd, vd, table.cuda(), 64, 0, scale, dv=dv,
+                                 out_dtype="f32", want_lse=True)
+    n = np.arange(hist + 1, hist + new + 1, dtype=np.float64)
+    want = 16 + np.log1p((n - 1) * np.exp(low - 16))
+    err = np.abs(lse.double().cpu().numpy() - want[:, None])
+    # scaling a logit rounds twice (2^-23 of 16), exponentials and logarithm 2^-20, the sum's own 2^-22, lse's rounding 2^-22 of it
+    assert (err <= 2.0 ** -23 * 16 * 2 + 2.0 ** -20 + 2.0 ** -22 + 2.0 ** -22 * want[:, None]).all(), err.max()
+    # the value 0.75: probabilities in bf16, and O's accumulators rounded once for 16 keys
+    got = out[..., 1].double().cpu().numpy()
+    assert (np.abs(got - 0.75) <= (2.0 ** -8 + n[:, None] / 16 * 2.0 ** -25 + 2.0 ** -18) * 0.75).all()
