@@ -169,6 +169,9 @@ constexpr bool mqa_shared(int64_t total_q, int64_t k)
 constexpr int PA_ROWS = 128;  // (token, head) rows of a block
 constexpr int PA_XCD = 8;
 constexpr int PA_CUS = 256;
+// Keys of a range at most.  A block's O is rounded to fp32 once for 16 keys: over n of them that score alike it
+// may be off by n / 16 * 2^-25 of sum p |v|, 2^-10 here (measured in one range: 2^-9 at 2^20 keys, 3% at 2^24).
+constexpr int PA_LONGEST = 1 << 19;
 constexpr int64_t PA_MAX_BLOCKS = (1 << 24) - 1;  // a launch takes fewer than 2^32 threads
 
 // First tile of session s's own rows, whose tokens start at q_start: each session has as
@@ -211,10 +214,10 @@ constexpr PrefixPlan prefix_plan(int num_seqs, int total_q, int max_q, int max_c
     p.one = heads % PA_ROWS != 0 && (int64_t)max_q * heads <= PA_ROWS;
     p.own_tiles = p.one ? num_seqs : prefix_tile_first(total_q, heads, num_seqs);
     // Whole rounds of blocks need no split; the last tiles are split over the round that is left.
-    const int64_t rounds = share ? 0 : apart / resident;
+    const int own = max_ctx - p.prefix;
+    const int64_t rounds = share || own > PA_LONGEST ? 0 : apart / resident;
     p.whole = (int)(rounds * resident * p.own_tiles / apart);
     const int64_t rest = apart - rounds * resident, ids = p.own_tiles - p.whole;
-    const int own = max_ctx - p.prefix;
     const int mean = total_ctx / num_seqs > p.prefix ? (int)(total_ctx / num_seqs) - p.prefix : 0;
     const int span = own > p.prefix ? own : p.prefix;
     // Time of a split, in keys of a block.  Blocks that all run at once take as long as the
@@ -254,11 +257,13 @@ constexpr PrefixPlan prefix_plan(int num_seqs, int total_q, int max_q, int max_c
         }
         return chunk == tile || work > 8.0 * resident;
     };
-    for (int n = 1; n <= 256 && !attempt(n); n += 1 + n / 16)
+    const int least = span / PA_LONGEST + (span % PA_LONGEST != 0);
+    const int first = least > 1 ? least : 1;
+    for (int n = first; (n == first || n <= 256) && !attempt(n); n += 1 + n / 16)
         ;
     // and as many as fill the chip once, with the own chunks as they are
     const double fill = share ? (room - (double)ids * p.own_chunks) / p.shared_tiles : room / (double)(ids > 0 ? ids : 1);
-    if (fill > 1.0)
+    if (fill > 1.0 && fill >= least)
         attempt((int)fill);
     p.slots = p.shared_chunks + p.own_chunks;
     if (p.slots == 1 || rest == 0) {

@@ -38,3 +38,35 @@ def test_the_sum_over_many_keys(rules, kind, heads, hist, new):  # noqa: F811
     # the value 0.75: probabilities in bf16, and O's accumulators rounded once for 16 keys
     got = out[..., 1].double().cpu().numpy()
     assert (np.abs(got - 0.75) <= (2.0 ** -8 + n[:, None] / 16 * 2.0 ** -25 + 2.0 ** -18) * 0.75).all()
+
+
+@pytest.mark.parametrize("kind,heads,new", [("mqa2", 16, 8192), ("mla", 128, 512)])
+def test_the_output_over_many_keys(kind, heads, new):
+    """Three million keys that score alike, at half the weight of the first: bf16 holds their probabilities, so
+    the output is off by the roundings of O alone, one for 16 keys of a range of at most 2^19, and by those of the
+    join (2^-18 with the exponentials')."""
+    dqk, dv = (576, 512) if kind == "mla" else (128, 128)
+    n, scale = 3 << 20, float(np.log(2) / 80)              # logits 16 * 16 and 16 * 11: ln 2 apart
+    g = torch.Generator()
+    g.manual_seed(0)
+    vals = (torch.rand(dv, generator=g) + 0.5).bfloat16()
+    k = torch.zeros((128, dqk), dtype=torch.bfloat16)
+    k[:, 0] = 11
+    k[0, 0] = 16
+    if kind == "mla":
+        k[:, 1:dv] = vals[1:]                              # (q has 0 there)
+    pools = [k.cuda()] * 2 if kind == "mla" else [k.cuda(), vals.repeat(128, 1).cuda()]
+    q = torch.zeros((new, heads, dqk), dtype=torch.bfloat16)
+    q[..., 0] = 16
+    table = torch.ones((1, n // 64), dtype=torch.int32)
+    table[0, 0] = 0
+    print("prefix long", kind, flush=True)
+    out, lse = janus.prefix_attn(janus.Batch([n - new], [new]), q.cuda(), *pools, table.cuda(), 64, 0, scale, dv=dv,
+                                 out_dtype="f32", want_lse=True)
+    want = vals.double().numpy()[1:]
+    err = np.abs(out[..., 1:].double().cpu().numpy() - want) / want
+    assert (err <= 2.0 ** -10 + 2.0 ** -18).all(), err.max()
+    ids = np.arange(n - new, n, dtype=np.float64)
+    wl = 256 * scale + np.log1p(ids / 2)
+    # a logit rounds twice in its scaling (2^-23 of 3.6 with log2 e: 5.2)
+    assert (np.abs(lse.double().cpu().numpy() - wl[:, None]) <= 2.0 ** -23 * 5.2 + 2.0 ** -20 + 2.0 ** -22 * (1 + wl[:, None])).all()
