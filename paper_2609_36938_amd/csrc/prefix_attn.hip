@@ -174,74 +174,95 @@ struct Total {
 };
 JANUS_DEV float sum8(v8f p) { return ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7])); }
 
-// The block's rows without matrix instructions: a wave a row, a lane a key, then DV / 64 dims.
-// For blocks that hold an infinity or NaN in a row of V of a tile in which rows end
-// at different keys: a probability of 0 does not undo it for the rows without the key.
-template <int DQK, int DV>
-JANUS_DEV void plain_rows(const PrefixArgs &g, const PrefixRange &r, const int *lim)
+// Values of V that are not finite, where rows end: a probability of 0 does not undo them for the rows
+// without the key, so the tiles in which rows end are searched for them, and the products take 0 in
+// their place.  What they give the rows that have the key is known without a product: any sum with them
+// is infinite or NaN.  (A block that was done again key by key for their sake, all 128 rows of it, took
+// minutes over long contexts: one overflowed row of the cache held up a batch.)
+JANUS_DEV bool not_finite(int x) { return ((x & 0x7f80) == 0x7f80) | ((x & 0x7f800000) == 0x7f800000); }
+JANUS_DEV bool not_finite(v4i x) { return not_finite(x[0]) | not_finite(x[1]) | not_finite(x[2]) | not_finite(x[3]); }
+JANUS_DEV v4i finite_or_0(v4i x)
 {
-    constexpr int N = DV / 64;
-    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        x[e] &= (x[e] & 0x7f80) == 0x7f80 ? (int)0xffff0000 : -1;
+        x[e] &= (x[e] & 0x7f800000) == 0x7f800000 ? 0xffff : -1;
+    }
+    return x;
+}
+constexpr int NEVER = 0x7fffffff;  // no tile, no key
+
+// Adds the values that are not finite of V's keys from `from` on, dims dim0 .. dim0 + 127, to rows
+// rbeg .. rend - 1 of O, which this wave has written; sixteen lanes a key, then a row.  ONE_POOL: V's rows are
+// K's, so the key's logit is infinite too, and its probability NaN, or 0, or makes all others 0: NaN in
+// every case.  With pools apart that is so where the key's row of K is not finite either.
+template <int DV, bool ONE_POOL>
+JANUS_DEV void add_not_finite(const PrefixArgs &g, const PrefixRange &r, const int *lim, int from, int dim0, int rbeg,
+                              int rend)
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "workgroup");  // (other lanes' stores)
+    const int lane = threadIdx.x & 63, in = lane & 15, group = lane >> 4;
     const int32_t *pt = g.table + (int64_t)r.sess * g.pt_ld;
-    auto slot = [&](int key) {
-        return ((int64_t)pt[key >> g.page_shift] << g.page_shift) + (key & ((1 << g.page_shift) - 1));
-    };
-    for (int row = r.row0 + (threadIdx.x >> 6); row < r.row1; row += PA_WAVES) {
-        const uint16_t *q = g.q + (int64_t)row * DQK;
+    int plus[8], minus[8];  // the first keys with +inf and -inf, or NaN, of eight dims
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        plus[e] = minus[e] = NEVER;
+    constexpr int AHEAD = 4;
+    for (int k0 = max(from, r.kbeg); k0 < r.kend; k0 += 4 * AHEAD) {
+        int64_t slot[AHEAD];
+        v4i x[AHEAD];
+        bool hit = false;
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) {
+            const int key = min(k0 + 4 * a + group, r.kend - 1);
+            slot[a] = ((int64_t)pt[key >> g.page_shift] << g.page_shift) + (key & ((1 << g.page_shift) - 1));
+            x[a] = *(const v4i *)(g.v + slot[a] * g.v_rb + 2 * dim0 + 16 * in);
+            hit |= not_finite(x[a]);
+        }
+        if (__ballot(hit) == 0)
+            continue;
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) {
+            const int key = min(k0 + 4 * a + group, r.kend - 1);
+            bool both = ONE_POOL;
+            if (!ONE_POOL)
+                both = (__ballot(not_finite(*(const v4i *)(g.k + slot[a] * g.k_rb + 16 * in))) >> (16 * group) & 0xffff) != 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const uint32_t v = (uint32_t)x[a][e / 2] >> (16 * (e % 2)) & 0xffff;
+                if ((v & 0x7f80) != 0x7f80)
+                    continue;
+                const bool nan = both || (v & 0x7f) != 0;
+                if (nan || v < 0x8000)
+                    plus[e] = min(plus[e], key);
+                if (nan || v >= 0x8000)
+                    minus[e] = min(minus[e], key);
+            }
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int o = 16; o < 64; o <<= 1) {
+            plus[e] = min(plus[e], __shfl_xor(plus[e], o));
+            minus[e] = min(minus[e], __shfl_xor(minus[e], o));
+        }
+    for (int row = rbeg + group; row < rend; row += 4) {
         const int end = lim[row - r.row0];
-        float m = M_INIT, acc[N] = {};
-        Total sum = {0.f, 0.f};
-        for (int k0 = r.kbeg; k0 < end; k0 += 64) {
-            float x = -INFINITY;
-            if (k0 + lane < end) {
-                const uint16_t *k = (const uint16_t *)(g.k + slot(k0 + lane) * g.k_rb);
-                x = 0.f;
-                for (int e = 0; e < DQK; ++e)
-                    x = fmaf(bf16_to_f32(q[e]), bf16_to_f32(k[e]), x);
-                x *= g.scale_log2;
-            }
-            float top = x;
 #pragma unroll
-            for (int o = 1; o < 64; o <<= 1)
-                top = fmaxf(top, __shfl_xor(top, o));
-            const float mnew = fmaxf(m, top), alpha = __builtin_amdgcn_exp2f(m - mnew);
-            m = mnew;
-            const float p = k0 + lane < end ? __builtin_amdgcn_exp2f(x - m) : 0.f;
-            sum.scale(alpha);
-            float tile = p;
-#pragma unroll
-            for (int o = 1; o < 64; o <<= 1)
-                tile += __shfl_xor(tile, o);
-            sum.add(tile);
-#pragma unroll
-            for (int e = 0; e < N; ++e)
-                acc[e] *= alpha;
-            for (int j = 0; j < min(64, end - k0); ++j) {
-                const float pj = __shfl(p, j);
-                const uint16_t *v = (const uint16_t *)(g.v + slot(k0 + j) * g.v_rb) + N * lane;
-#pragma unroll
-                for (int e = 0; e < N; ++e)
-                    acc[e] = fmaf(pj, bf16_to_f32(v[e]), acc[e]);
-            }
-        }
-        const int64_t at = r.part + (row - r.row0);
-        const float l = sum.sum;
-        const float inv = l != 0.f ? 1.f / l : 0.f;
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const int64_t o = (int64_t)row * DV + N * lane + e;
+        for (int e = 0; e < 8; ++e) {
+            const bool up = plus[e] < end, down = minus[e] < end;
+            if (!up && !down)
+                continue;
+            const float x = up && down ? NAN : up ? INFINITY : -INFINITY;
+            const int dim = dim0 + 8 * in + e;
+            const int64_t o = (int64_t)row * DV + dim;
             if (r.part >= 0)
-                g.part[at * DV + N * lane + e] = acc[e];
+                g.part[(r.part + (row - r.row0)) * DV + dim] += x;
             else if (g.out_f32)
-                ((float *)g.out)[o] = acc[e] * inv;
+                ((float *)g.out)[o] += x;
             else
-                ((__bf16 *)g.out)[o] = (__bf16)(acc[e] * inv);
-        }
-        if (lane == 0) {
-            if (r.part >= 0)
-                *(float2 *)(g.part + g.plan.slots * g.plan.part_rows * DV + 2 * at) = float2{m, l};
-            else if (g.lse)
-                g.lse[row] = l != 0.f ? (m + log2f(l)) * LN2 : -INFINITY;
+                ((__bf16 *)g.out)[o] = (__bf16)((float)((__bf16 *)g.out)[o] + x);
         }
     }
 }
@@ -302,8 +323,8 @@ __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
             o[d][i] = 0.f;
     float m = M_INIT;
     Total lsum = {0.f, 0.f};
-    int bad = 0;   // a tile where rows end holds values of V that are not finite
-    int bmin = 0;  // keys before it are every row's
+    int bad = NEVER;  // the first tile where rows end whose V is not finite, in this wave's share of it
+    int bmin = 0;     // keys before it are every row's
 
     // Tiles begin at multiples of their length: a tile of longer pages lies in one.
     // A wave gathers four rows at a time, rows 16 j + 4 wave .. of K and of V.
@@ -382,7 +403,8 @@ __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
         const uint8_t *vt = ring + SLOT * BUF + KBUF;
         const int base = base0 + t * PQ_KT;
         float mult = g.scale_log2;
-        if (base < kbeg || base + PQ_KT > bmin || mult <= 0.f) {
+        const bool ragged = base < kbeg || base + PQ_KT > bmin;
+        if (ragged || mult <= 0.f) {
             // keys 8 (i / 4) + 4 hf + i % 4 of this lane's row
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -390,13 +412,17 @@ __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
                 s[i] = key >= kbeg && key < lim ? s[i] * mult : -INFINITY;
             }
             mult = 1.f;
-#pragma unroll
-            for (int w = 0; w < KBUF / 1024; w += PA_WAVES) {  // (every wave comes here)
-                const v4i x = *(const v4i *)(vt + 1024 * (w + wave) + 16 * lane);
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    bad |= (x[e] & 0x7f80) == 0x7f80 || (x[e] & 0x7f800000) == 0x7f800000;
+        }
+        if (ragged) {  // (every wave comes here, with a share of the tile)
+            uint8_t *share = ring + SLOT * BUF + KBUF + 1024 * wave + 16 * lane;
+            static_assert(KBUF == 2 * 1024 * PA_WAVES, "two pieces a wave");
+            const v4i x = *(const v4i *)share, y = *(const v4i *)(share + 1024 * PA_WAVES);
+            if (__ballot(not_finite(x) | not_finite(y)) != 0) {
+                *(v4i *)share = finite_or_0(x);
+                *(v4i *)(share + 1024 * PA_WAVES) = finite_or_0(y);
+                bad = min(bad, t);
             }
+            lds_barrier();
         }
         float mx = s[0];
 #pragma unroll
@@ -477,23 +503,13 @@ __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
         }
     }
 
-    const int mine = __ballot(bad) != 0;
     if (lane == 0)
-        sBad[wave] = mine;
+        sBad[wave] = bad;
     const float l = lsum.sum + __shfl_xor(lsum.sum, 32);
     lds_barrier();
     const v4i any = *(const v4i *)sBad;
-    if (__builtin_amdgcn_readfirstlane(any[0] | any[1] | any[2] | any[3])) {
-        __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
-        plain_rows<128, 128>(g, r, sLim);
-        return;
-    }
-    // (the gathers behind the last tile still write LDS: a wave waits for its own before it ends)
-    if (!live) {
-        __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
-        return;
-    }
-    if (r.part >= 0) {
+    const int first = __builtin_amdgcn_readfirstlane(min(min(any[0], any[1]), min(any[2], any[3])));
+    if (live && r.part >= 0) {
         const int64_t at = r.part + (row - r.row0);
         if (hf == 0)
             *(float2 *)(g.part + g.plan.slots * g.plan.part_rows * 128 + 2 * at) = float2{m, l};
@@ -505,19 +521,23 @@ __global__ __launch_bounds__(PA_THREADS, 2) void prefix_mqa(PrefixArgs g)
                     *(v4f *)(g.part + at * 128 + 32 * d + 2 * i + 4 * hf) =
                         v4f{o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
         }
-        __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
-        return;
+    } else if (live) {
+        const float inv = l != 0.f ? 1.f / l : 0.f;
+#pragma unroll
+        for (int d = 0; d < NB; ++d)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4)
+                store_out4(g.out, g.out_f32, (int64_t)row * 128 + 32 * d + 2 * i + 4 * hf,
+                           v4f{o[d][i] * inv, o[d][i + 1] * inv, o[d][i + 2] * inv, o[d][i + 3] * inv});
+        if (g.lse && hf == 0)
+            g.lse[row] = l != 0.f ? (m + log2f(l)) * LN2 : -INFINITY;
     }
-    const float inv = l != 0.f ? 1.f / l : 0.f;
-#pragma unroll
-    for (int d = 0; d < NB; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; i += 4)
-            store_out4(g.out, g.out_f32, (int64_t)row * 128 + 32 * d + 2 * i + 4 * hf,
-                       v4f{o[d][i] * inv, o[d][i + 1] * inv, o[d][i + 2] * inv, o[d][i + 3] * inv});
-    if (g.lse && hf == 0)
-        g.lse[row] = l != 0.f ? (m + log2f(l)) * LN2 : -INFINITY;
+    // the gathers behind the last tile still write LDS: a wave waits for its own before it ends
     __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
+    if (first != NEVER) {
+        const int r0 = r.row0 + 32 * wave;
+        add_not_finite<128, false>(g, r, sLim, base0 + first * PQ_KT, 0, r0, min(r0 + 32, r.row1));
+    }
 }
 
 constexpr int PM_KT = 32, PM_STEPS = 576 / 16;
@@ -565,6 +585,7 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
     __shared__ __attribute__((aligned(16))) uint8_t main_ring[4 * PM_MAIN], tail_ring[3 * PM_TAIL];
     __shared__ v4i sP[2][PA_WAVES][2][64];       // probabilities of the waves' rows, as operands
     __shared__ v4i sOver;                        // a wave's rows outgrew their maxima
+    __shared__ int sBad[PA_WAVES];               // the first tile that a wave has cleaned
     __shared__ int sLim[PA_ROWS];
     __shared__ float sM[PA_ROWS], sL[PA_ROWS];
 
@@ -581,6 +602,8 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
     const int lim = row_limit(g, r, live ? row : r.row1 - 1);
     if (hf == 0)
         sLim[32 * wave + c32] = lim;
+    if (lane == 0)
+        sBad[wave] = NEVER;
 
     v8bf qf[PM_STEPS];
     {
@@ -722,6 +745,10 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
             __builtin_amdgcn_sched_barrier(0);
         }
     };
+    // Four keys of the wave's dims of a tile (the other waves score them, and do not multiply them).
+    auto own_dims = [&](int t, int w) {
+        return (v4i *)(main_ring + (t & 3) * PM_MAIN + 1024 * (4 * w + (lane >> 4)) + 256 * wave + 16 * (lane & 15));
+    };
     // The logits of tile t scaled, those of keys that a row does not have -inf;
     // returns the factor that is left to apply.
     auto mask = [&](int t) {
@@ -736,16 +763,22 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
             s[i] = key >= kbeg && key < lim ? s[i] * g.scale_log2 : -INFINITY;
         }
         if (!inside) {
-            const uint8_t *tile = main_ring + (t & 3) * PM_MAIN;
 #pragma unroll 2
-            for (int w = 0; w < 8; ++w) {
-                const v4i x = *(const v4i *)(tile + 1024 * (4 * w + (lane >> 4)) + 256 * wave + 16 * (lane & 15));
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    bad |= (x[e] & 0x7f80) == 0x7f80 || (x[e] & 0x7f800000) == 0x7f800000;
-            }
+            for (int w = 0; w < 8; ++w)
+                bad |= not_finite(*own_dims(t, w));
         }
         return 1.f;
+    };
+    // Once a wave has found such values, it takes them out of its dims of every tile that it multiplies,
+    // when the tile has been scored.
+    auto clean = [&](int t) {
+        if (__ballot(bad) == 0)
+            return;
+#pragma unroll 1
+        for (int w = 0; w < 8; ++w)
+            *own_dims(t, w) = finite_or_0(*own_dims(t, w));
+        if (lane == 0)
+            sBad[wave] = min(sBad[wave], t);
     };
     // Probabilities of s * mult (mult > 0), relative to the maximum of the first
     // tile that has keys of the row.
@@ -799,6 +832,7 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
             for (int t = 1; t < nt; ++t) {
                 // (behind the last tile the gathers read its last key again)
                 const int next = SMALL ? 0 : entry(t + 3);
+                clean(t - 1);
                 if (SMALL)
                     issue(t + 2);
                 logits(t, std::integral_constant<int, PM_WITH>{}, page);
@@ -818,6 +852,7 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
                 }
                 give(t);
             }
+            clean(nt - 1);
             product_begin(nt - 1);
 #pragma unroll
             for (int j = 0; j < 32; ++j)
@@ -860,12 +895,6 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
         __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
     }
 
-    // Rows that end in a tile whose V holds an infinity or NaN: a probability of 0
-    // does not undo it.  The block is done again, a row and a key at a time.
-    if (__syncthreads_or(bad)) {
-        plain_rows<576, 512>(g, r, sLim);
-        return;
-    }
     const float l = lsum.sum + __shfl_xor(lsum.sum, 32);
     if (hf == 0) {
         sM[32 * wave + c32] = m;
@@ -905,6 +934,8 @@ __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)
         if (g.lse && hf == 0 && wave == 0)
             g.lse[to] = ll != 0.f ? (mm + log2f(ll)) * LN2 : -INFINITY;
     }
+    if (__ballot(bad) != 0)
+        add_not_finite<512, true>(g, r, sLim, base0 + sBad[wave] * PM_KT, 128 * wave, r.row0, r.row1);
 }
 
 // Joins the ranges of a row: with maxima m_s and sums l_s, M = max m_s and w_s =
