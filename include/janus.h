@@ -445,10 +445,12 @@ typedef struct {
 /*
  * Frequencies of a rotary embedding (host only: inv_freq is host memory, dim/2
  * doubles; nothing is enqueued).  Pair j turns base^(-2j/dim) a position.
- * JANUS_SCALING_LINEAR divides all frequencies by factor.  JANUS_SCALING_YARN
- * (Peng et al., arXiv 2309.00071) keeps those that make more than beta_fast
- * turns over original_ctx positions, divides those that make fewer than
- * beta_slow, goes from one to the other linearly in j, and sets magnitude to
+ * JANUS_SCALING_LINEAR divides all frequencies by factor.  JANUS_SCALING_YARN keeps
+ * the fast ones, divides the slow ones by factor, and goes from one to the other in
+ * a straight line of j, the form that released checkpoints use (the paper, Peng et al., arXiv
+ * 2309.00071, has the line in the number of turns): with p(t) the fractional j whose
+ * frequency makes t turns over original_ctx positions, from j = max(floor(p(beta_fast)), 0)
+ * to min(ceil(p(beta_slow)), dim - 1).  It sets magnitude to
  * 0.1 ln(factor) + 1 (else 1).  The arguments that a kind does not use are
  * ignored (factor must be >= 1 all the same).
  */
