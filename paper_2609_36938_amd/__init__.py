@@ -399,18 +399,16 @@ def _at(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
-def _no_gradient(what: str, *tensors):
-    """The calls record nothing for autograd: a tensor that it follows is refused rather than cut off from it."""
+def _followed(what: str):
+    """A tensor of the call requires a gradient.  The calls record nothing for autograd: they refuse a tensor that it
+    follows rather than cut it off."""
     if torch.is_grad_enabled():
-        for t in tensors:
-            if t is not None and t.requires_grad:
-                raise JanusError(f"{what}: a gradient would be lost here; call under torch.no_grad(), or in the forward "
-                                 "and backward functions of a torch.autograd.Function")
+        raise JanusError(f"{what}: a gradient would be lost here; call under torch.no_grad(), or in the forward "
+                         "and backward functions of a torch.autograd.Function")
 
 
-def _written(*tensors):
-    """Tensors of the caller's that a call has written: a graph that keeps one for its backward pass will notice."""
-    torch.autograd.graph.increment_version([t for t in tensors if t is not None])
+# A tensor of the caller's has been written: a graph that keeps it for its backward pass will notice.
+_written = torch.autograd.graph.increment_version
 
 
 def _empty(dtype, device, stream, *shape):
@@ -525,7 +523,7 @@ def page_grow(batch: Batch, page_size: int, free_list, page_table, free_head=Non
     _launch(what, dev, stream, lib().janus_page_grow, batch.ref, page_size, free_list.data_ptr(), free_list.numel(),
             _at(free_head), page_table.data_ptr(), _table(batch, page_table, page_size),
             slots.data_ptr() if total else at, at)
-    _written(page_table, slots, counts)
+    _written(page_table if out is None else [page_table, slots, counts])
     return page_table, slots, counts
 
 
@@ -562,6 +560,9 @@ def rope(batch: Batch, rotary: Rotary, x, out=None, out_dtype: Optional[str] = N
     if out_dtype not in _ROPE_OUT:
         raise JanusError(f"{what}: unknown out_dtype {out_dtype!r}")
     odt, torch_dt = _ROPE_OUT[out_dtype]
+    given, given_scale = out, out_scale
+    if x.requires_grad or (out is not None and out.requires_grad):
+        _followed(what)
     if out is None:
         out = _empty(torch_dt, x.device, stream, *shape)
     elif out.dtype is not torch_dt and not (out_dtype == "fp8" and out.dtype is torch.float8_e4m3fn):
@@ -574,16 +575,20 @@ def rope(batch: Batch, rotary: Rotary, x, out=None, out_dtype: Optional[str] = N
             out_scale = _empty(torch.float32, x.device, stream, total)
         else:
             _want(what, "out_scale", out_scale, torch.float32, total)
+            if out_scale.requires_grad:
+                _followed(what)
     elif out_scale is not None:
         raise JanusError(f"{what}: out_scale goes with fp8 outputs")
     if rotary.positions is not None:
         rotary._check(what, batch)
-    _no_gradient(what, x, out, out_scale)
     dev = _device(what, x, out, out_scale, batch.q_start, rotary.inv_freq)
     if total:
         _launch(what, dev, stream, lib().janus_rope, batch.ref, rotary.ref, x.data_ptr(), xdt, xs[0], xs[1], shape[1],
                 shape[2], out.data_ptr(), odt, os_[0], os_[1], _at(out_scale))
-        _written(out, out_scale)
+        if given is not None:
+            _written(given)
+        if given_scale is not None:
+            _written(given_scale)
     return out, out_scale
 
 
@@ -605,6 +610,8 @@ def kv_append(batch: Batch, x, out, rotary: Optional[Rotary] = None, x_rot=None,
             if len(shape) != 2 or shape[0] != total or t.dtype is not given.dtype or (shape[1] > 1 and t.stride(1) != 1):
                 raise JanusError(f"{what}: x and x_rot are to be [{total}, elements] of one type, elements adjacent")
             n += shape[1]
+            if t.requires_grad:
+                _followed(what)
     if given is None or (x_rot is not None and (rotary is None or x_rot.shape[1] != rotary.dim)):
         raise JanusError(f"{what}: x, or x_rot with the elements that rotary turns, or both")
     xdt, odt = _float_code(what, "x", given), _dtype_code(out, None)
@@ -621,15 +628,16 @@ def kv_append(batch: Batch, x, out, rotary: Optional[Rotary] = None, x_rot=None,
             raise JanusError(f"{what}: out_scale goes with fp8 rows")
         if out_scale.dtype is not torch.float32 or not out_scale.is_contiguous() or out_scale.numel() != num_rows:
             raise JanusError(f"{what}: out_scale is to hold one float32 for each of {num_rows} rows")
+    if out.requires_grad or (out_scale is not None and out_scale.requires_grad):
+        _followed(what)
     if rotary is not None and rotary.positions is not None:
         rotary._check(what, batch)
-    _no_gradient(what, x, x_rot, out, out_scale)
     dev = _device(what, out, x, x_rot, rows, out_scale, batch.q_start, None if rotary is None else rotary.inv_freq)
     if total:
         _launch(what, dev, stream, lib().janus_kv_append, batch.ref, None if rotary is None else rotary.ref, _at(x),
                 xdt, 0 if x is None else x.stride(0), _at(x_rot), 0 if x_rot is None else x_rot.stride(0), n,
                 _at(rows), num_rows, out.data_ptr(), odt, width * out.element_size(), _at(out_scale))
-        _written(out, out_scale)
+        _written(out if out_scale is None else [out, out_scale])
     return out
 
 
@@ -673,6 +681,7 @@ def prefix_attn(batch: Batch, q, k_pool, v_pool, page_table, page_size: int, pre
         raise JanusError(f"{what}: prefix_len is to be 0 to {batch.max_ctx}, not {prefix_len}")
     _want(what, "page_table", page_table, torch.int32, batch.c.num_seqs, None)
     odt, torch_dt = (JANUS_BF16, bf16) if out_dtype == "bf16" else (JANUS_F32, torch.float32)
+    given, given_lse = out, lse
     if out is None:
         out = _empty(torch_dt, dev, stream, total, Hq, dv)
     else:
@@ -681,7 +690,9 @@ def prefix_attn(batch: Batch, q, k_pool, v_pool, page_table, page_size: int, pre
         _want(what, "lse", lse, torch.float32, total, Hq)
     elif want_lse:
         lse = _empty(torch.float32, dev, stream, total, Hq)
-    _no_gradient(what, q, k_pool, v_pool, out, lse)
+    if q.requires_grad or k_pool.requires_grad or v_pool.requires_grad or out.requires_grad or (
+            lse is not None and lse.requires_grad):
+        _followed(what)
     index = _device(what, q, k_pool, v_pool, page_table, out, lse, workspace, batch.q_start)
     if total == 0:
         return out, lse
@@ -689,10 +700,15 @@ def prefix_attn(batch: Batch, q, k_pool, v_pool, page_table, page_size: int, pre
     args = (batch.ref, q.data_ptr(), Hq, dqk, dv, k_pool.data_ptr(), v_pool.data_ptr(), krs, vrs, page_table.data_ptr(),
             _table(batch, page_table, page_size), page_size, prefix_len, scale, out.data_ptr(), odt, _at(lse))
     if workspace is None:
-        need = ctypes.c_size_t(0)
-        _check(fn(*args, None, ctypes.byref(need), None), what)
-        workspace = _empty(torch.uint8, dev, stream, max(need.value, 1))
-    at, size = _workspace(workspace, out)
+        size = ctypes.c_size_t(0)
+        _check(fn(*args, None, ctypes.byref(size), None), what)
+        workspace = _empty(torch.uint8, dev, stream, max(size.value, 1))
+        at = workspace.data_ptr()
+    else:
+        at, size = _workspace(workspace, out)
     _launch(what, index, stream, fn, *args, at, ctypes.byref(size))
-    _written(out, lse)
+    if given is not None:
+        _written(given)
+    if given_lse is not None:
+        _written(given_lse)
     return out, lse
