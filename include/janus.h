@@ -534,6 +534,9 @@ int janus_kv_append(const janus_batch *b, const janus_rotary *r, const void *x, 
  * no candidate gets out = 0 and lse = -inf.  Rows from q_start[B] on are left as
  * they are.  Ids that a token does not attend to do not touch its result,
  * whatever their rows hold.
+ * Logits, maxima, sums and products are fp32; probabilities are rounded to bf16 before they
+ * multiply V, for fp32 outputs too: an output is within 2^-8 of sum p |v|, and 2^-10 more
+ * over the longest contexts, beside the logits' own roundings and its rounding to out_dt.
  */
 int janus_prefix_attn(const janus_batch *b, const void *q, int Hq, int dqk, int dv,
                       const void *k_pool, const void *v_pool,

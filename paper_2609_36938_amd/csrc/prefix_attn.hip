@@ -16,7 +16,8 @@
 //   * Ranges of one row are joined by their maxima and sums (prefix_combine): few rows
 //     have too few blocks for 256 CUs otherwise.
 // Logits, maxima, sums and O are fp32.  Probabilities are rounded to bf16, the type of
-// the V that they multiply; their sums are taken before that.  The error is 2^-8 of the
+// the V that they multiply (in two parts they would take twice the MFMAs), also where the output
+// is fp32; their sums are taken before that.  The error is 2^-8 of the
 // values at most for each key, and mostly averages out (2.2e-3 of the result
 // with 4096 keys, 1.7e-3 of it the rounding of the result to bf16).
 //
@@ -278,10 +279,11 @@ constexpr int PQ_KT = 32;  // keys of a tile
 
 // MQA, 128 dims.  A tile is 8 MFMAs for S^T and 8 for O^T in each wave, 512 cycles, and
 // 16 exponentials a lane: those go under the MFMAs that score the next tile.  What bounds
-// it: long contexts, the MFMAs and what is not under them (2 sessions of 1000 to
-// 2000 tokens x 16 heads on 31000 ids: 775 to 810 us, 1.0 PFLOP/s; scores and exponentials one after
-// the other 10% more); few rows, the chain of loads before the first tile (2.4 us), a loop of
-// few tiles, and the launch of the join (16 sessions x 8 heads on 4096 ids: 10.4 us).  32
+// it: long contexts, LDS, from which every wave reads the whole tile, 16 KB for its 16 MFMAs: eight waves
+// of a CU 128 KB in the 1024 cycles that their MFMAs take, all that LDS gives beside the gathers' writes
+// (2 sessions of 1000 to 2000 tokens x 16 heads on 31000 ids: 790 to 835 us, box by box, 1.0 PFLOP/s;
+// scores and exponentials one after the other 10% more); few rows, the chain of loads before the first
+// tile (2.4 us), a loop of few tiles, and the launch of the join (16 sessions x 8 heads on 4096 ids: 10 us).  32
 // keys a tile and 66 KB of LDS let two blocks share a CU, so that one's waits are the
 // other's work: the first form took 1740 us for the long case with 64 keys and one block a
 // CU, 1190 with this.  Four buffers, and a turn for each of them, keep LDS offsets constant.
@@ -568,14 +570,17 @@ JANUS_DEV void settled(v16f &s) { asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s));
 // accumulators, which leaves 256 registers for 144 of queries and the operands.
 // While tile t is scored, tile t - 1 is multiplied: PM_WITH of its steps stand among the chain's, the
 // others under the exponentials (the longest case below 7.77 ms with 8 steps, 7.40 with 16, 7.43 with
-// 24, on one card).  What bounds it is the rate of the MFMAs at the power the chip has: 1.16 to
-// 1.22 PFLOP/s on long ranges (8 sessions of 100 to 300 tokens x 128 heads on 17000 ids, 6.6 to
-// 6.9 ms), where a library product of 8192^3 reaches 1.22 and of 16384^3 1.40; they are busy in
-// 55% of the cycles.  Few rows pay 5 to 8 us before the first tile (queries and tiles from HBM), as
-// much behind the last, and the join: 32 sessions x 16 heads on 131072 ids take 163 us where
-// the product's rate would take 105.  The first form, with each wave's O^T rescaled
-// as maxima grow, spilled it and took 95 ms for the longest case; gathers left out behind the last
-// tile, by a branch, cost 7%.
+// 24, on one card).  1.10 to 1.24 PFLOP/s on long ranges (8 sessions of 100 to 300 tokens x 128 heads on
+// 17000 ids, 6.5 to 7.3 ms, box by box), where a library product of 8192^3 reaches 1.22 and of 16384^3
+// 1.40.  The MFMAs are busy in 54% of the cycles; between them lie the scoring chain's dependences, the
+// exchange of probabilities and a barrier a tile.  Few rows pay 5 to 8 us before the first tile (queries
+// and tiles from HBM), as much behind the last, and the join: 32 sessions x 16 heads on 131072 ids take
+// 163 to 185 us where the product's rate would take 105.  47 registers are spilled, 30 dwords a lane in all: in the
+// loop one is read back a tile; the others are written before the loop and in the epilogue, which takes O
+// out of the accumulators.  The first form, with each wave's O^T rescaled
+// as maxima grow, spilled O itself and took 95 ms for the longest case; gathers left out behind the last
+// tile, by a branch, cost 7%.  A block whose logits outgrow its first tile's by 2^32 is done again, 2.5 to 2.7 times
+// the work: logits of a standard deviation of 4 nats do not (6.53 ms), of 16 nats do (17.5).
 // SMALL: pages of fewer than eight ids, where a wave's eight rows lie in different ones.
 template <bool SMALL>
 __global__ __launch_bounds__(PA_THREADS, 1) void prefix_mla(PrefixArgs g)

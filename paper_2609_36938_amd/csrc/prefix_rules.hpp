@@ -66,10 +66,10 @@ constexpr PrefixPlan prefix_plan(int num_seqs, int total_q, int max_q, int max_c
     // empty ones are not all taken again.  Without them counted, up to 4/5.)  An MQA
     // block beside another on its CU adds a third of its time.  Each block starts for 64 keys,
     // and a range of a row costs a hundredth of a key to write and read again.  Fitted
-    // to 35 batches of 1 to 100 sessions; of 39 batches on the kernels as they are, each with 27
-    // chunk lengths, the chunk taken is 0.5% off the best one in the mean for MLA and
-    // 2.6% for MQA, 10% at most (whole rounds of blocks, a start of 128 or 256 keys and a
-    // join of 0.02 or 0.01: 6 and 13% in the mean of the first 18).
+    // to 35 batches of 1 to 100 sessions.  Of 39 batches, each timed with 27 chunk lengths too, the
+    // plan's time is 2.7% off the shortest in the mean for MLA and 3.7% for MQA, 15% at most (three
+    // MQA batches and one of MLA by 9% and more); the shortest of 27 times is itself low by their scatter.  (Whole
+    // rounds of blocks, a start of 128 or 256 keys and a join of 0.02 or 0.01: 6 and 13% in the mean of 18.)
     const double start = 64, join = 0.01, tail = 0.5, slack = 0.8, beside = mla ? 0.0 : 0.35;
     const double room = (mla && heads % PA_ROWS != 0 && !p.one ? 0.94 : 1.0) * resident;
     double best = -1.0;

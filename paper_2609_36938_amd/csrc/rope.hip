@@ -20,10 +20,10 @@
 // angles are worked out.
 //
 // Bound by the bytes read and written where there are many (8192 tokens x 128 heads x 64 rotated
-// dims of bf16, 268 MB: 58 us, 4.6 TB/s; 2048 tokens x 64 heads x 128 dims to fp8, 50 MB: 11.4 us),
-// by one chain of loads (the session, its length, the frequencies' angles, the slot) where there are
-// few (16 decode queries 3.6 us, 64 cache rows to fp8 4.1; an empty kernel takes 2.5).  Loads behind
-// branches, which wait for each other: 71 us for the first of these.
+// dims of bf16, 268 MB: 58 us, 4.6 TB/s; 2048 tokens x 64 heads x 128 dims to fp8, 50 MB: 12.0 us, of
+// which 0.5 are the corrections of the quotients), by one chain of loads (the session, its length, the
+// frequencies' angles, the slot) where there are few (16 decode queries 3.7 us, 64 cache rows to fp8
+// 4.2; an empty kernel takes 2.5).  Loads behind branches, which wait for each other: 71 us for the first of these.
 #include "janus_device.hpp"
 #include "janus_host.hpp"
 
