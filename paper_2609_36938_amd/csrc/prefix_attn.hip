@@ -281,7 +281,7 @@ constexpr int PQ_KT = 32;  // keys of a tile
 // 16 exponentials a lane: those go under the MFMAs that score the next tile.  What bounds
 // it: long contexts, LDS, from which every wave reads the whole tile, 16 KB for its 16 MFMAs: eight waves
 // of a CU 128 KB in the 1024 cycles that their MFMAs take, all that LDS gives beside the gathers' writes
-// (2 sessions of 1000 to 2000 tokens x 16 heads on 31000 ids: 790 to 835 us, box by box, 1.0 PFLOP/s;
+// (2 sessions of 1000 to 2000 tokens x 16 heads on 31000 ids: 790 to 835 us, card by card, 1.0 PFLOP/s;
 // scores and exponentials one after the other 10% more); few rows, the chain of loads before the first
 // tile (2.4 us), a loop of few tiles, and the launch of the join (16 sessions x 8 heads on 4096 ids: 10 us).  32
 // keys a tile and 66 KB of LDS let two blocks share a CU, so that one's waits are the
@@ -571,7 +571,7 @@ JANUS_DEV void settled(v16f &s) { asm volatile("s_nop 15\n\ts_nop 7" : "+v"(s));
 // While tile t is scored, tile t - 1 is multiplied: PM_WITH of its steps stand among the chain's, the
 // others under the exponentials (the longest case below 7.77 ms with 8 steps, 7.40 with 16, 7.43 with
 // 24, on one card).  1.10 to 1.24 PFLOP/s on long ranges (8 sessions of 100 to 300 tokens x 128 heads on
-// 17000 ids, 6.5 to 7.3 ms, box by box), where a library product of 8192^3 reaches 1.22 and of 16384^3
+// 17000 ids, 6.5 to 7.3 ms, card by card), where a library product of 8192^3 reaches 1.22 and of 16384^3
 // 1.40.  The MFMAs are busy in 54% of the cycles; between them lie the scoring chain's dependences, the
 // exchange of probabilities and a barrier a tile.  Few rows pay 5 to 8 us before the first tile (queries
 // and tiles from HBM), as much behind the last, and the join: 32 sessions x 16 heads on 131072 ids take
